@@ -14,12 +14,12 @@
  *
  * Conventions shared by every call
  * --------------------------------
- * - head_dim must be 128 and window 32; 1 <= num_q_heads / num_kv_heads <= 8 with
+ * - head_dim must be 128 and window 32; 1 <= num_q_heads / num_kv_heads <= 8 (16 for the 8-bit cache) with
  *   num_q_heads a multiple of num_kv_heads (query head j reads KV head j / G).
  * - Every array argument named "device" is device memory of the current HIP device, caller
  *   owned and 16-byte aligned. fp16 data is passed as uint16_t bit patterns (IEEE binary16).
- * - The library allocates no memory, keeps no state between calls and (except okvq_cache_status)
- *   never synchronizes and never copies between host and device: each call validates its
+ * - The library allocates no memory, keeps no state between calls and (except okvq_cache_status
+ *   and okvq_q8_status) never synchronizes and never copies between host and device: each call validates its
  *   arguments on the host and then enqueues kernels on `stream` (a hipStream_t; NULL is the
  *   default stream).
  * - Argument errors are detected before anything is enqueued: the call returns a negative
@@ -449,6 +449,178 @@ okvq_status okvq_decode_attention_dense(const okvq_dims* dims, const uint16_t* k
                                         const int32_t* seq_lens, const int32_t* lens_host, const uint16_t* q,
                                         float sm_scale, float* out, void* workspace, size_t workspace_bytes,
                                         void* stream, void* const* events);
+
+/* ---- Rotary positions on several axes --------------------------------------------------------
+ * Queries and keys are rotated by their positions before they are cached (the caches above and below
+ * hold rotated keys). Audio-visual streams have a position per axis (time, height, width): pair i of a
+ * row's 64 pairs of channels turns by the angle pos[axis[i]] * inv_freq[i],
+ *   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin),
+ * where a pair is channels (i, i + 64), or (2i, 2i + 1) with OKVQ_ROTARY_ADJACENT. The gradient of the
+ * rotation is the rotation by the opposite angle (OKVQ_ROTARY_INVERSE). */
+
+/* types of the rows of the calls below */
+enum { OKVQ_F16 = 0, OKVQ_BF16 = 1 };
+enum { OKVQ_ROTARY_INVERSE = 1u << 0, OKVQ_ROTARY_ADJACENT = 1u << 1 };
+
+typedef struct {               /* frequencies and axes, kept by the caller on the host */
+  double inv_freq[64];         /* radians per position of each pair (0 leaves a pair as it is) */
+  uint8_t axis[64];            /* 0..2: the position that turns the pair */
+} okvq_rotary_params;
+
+typedef struct {               /* rows of 128 channels: element (b, h, t, c) at data + b batch_stride + */
+  void* data;                  /* h head_stride + t token_stride + c. Strides in elements, multiples of 8 */
+  int64_t batch_stride, head_stride, token_stride; /* and not negative; data 16-byte aligned */
+} okvq_rows;
+
+/* Rotate queries and keys, from any row layout into any other (projections leave them token by token,
+ * the caches take them head by head), in one launch.
+ *   params     host
+ *   q, k       device rows [batch][q_heads or kv_heads][n_tokens], or NULL for none of the kind
+ *   positions  device i32 [batch][3][n_tokens], any values
+ *   lens_host  host i32 [batch], 0 <= lens_host[b] <= n_tokens: rows t < lens_host[b] are rotated, the
+ *              others are neither read nor written; NULL: all of them
+ *   q_out, k_out  device rows; an output may be its own input with the same strides (in place) and
+ *              may not overlap an input otherwise
+ *   dtype      OKVQ_F16 or OKVQ_BF16, of inputs and outputs
+ *   flags      OKVQ_ROTARY_INVERSE, OKVQ_ROTARY_ADJACENT
+ * The angle is formed as a 64-bit fraction of a turn, so that far positions lose nothing; the rotation
+ * is computed in fp32 and rounded once. 1 <= batch <= 65535, heads up to 65535 together. */
+okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                        int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const int32_t* positions,
+                        const int32_t* lens_host, const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype,
+                        uint32_t flags, void* stream);
+
+/* ---- Paged 8-bit cache --------------------------------------------------------------------------
+ * Keys and values in 8 bits with one scale for each block of 32 tokens and KV head, in pages that
+ * sequences share: a nearly lossless cache beside the packed one, for samples of one prompt and
+ * server batches. L layers, B sequence slots, H KV heads, P pages of T = page_tokens tokens:
+ *   k_codes  u8  [L][P][H][T][128]      token, channel
+ *   v_codes  u8  [L][P][H][T/32][4096]  block, byte 1024 j + 16 (16 g + n) + 8 b + 4 a + i: token
+ *                                       16 a + 4 g + i, channel 32 j + 16 b + n (the matrix cores'
+ *                                       operand order)
+ *   k_scale, v_scale  f32 [L][P][H][T/32]
+ *   k_stage, v_stage  [L][B][H][32][128] of the rows' type: raw rows of each slot's open block
+ *   block_table  i32 [B][max_pages]     pages of a slot in order (-1: none)
+ *   seq_lens     i32 [B]                tokens of a slot
+ *   page_refs    i32 [P]                slots that hold a page (0: free)
+ *   status       i32 [4]                word 0: 1 once okvq_q8_extend was short of pages (never cleared
+ *                                       by the library); word 1: pages in use after the last compaction
+ * A new cache has block_table -1 and the other four of these zero; nothing else needs contents.
+ * Codes: with amax the largest magnitude of the block's tokens and M = 127 (OKVQ_Q8_INT8) or 448
+ * (OKVQ_Q8_E4M3), scale = fl(amax * fl(1 / M)) in fp32 (1 where that is 0), t = fl(x / scale) clamped to
+ * +-M, and the code is rint(t) (two's complement) or t rounded to e4m3, both to nearest even. It stands for code *
+ * scale. Slots of a block behind the last token hold code 0. The order is a bit-exact contract, and a
+ * block that grows is quantized again from its raw rows: codes do not depend on the chunks in which
+ * tokens arrived.
+ * Tables, lengths and reference counts live on the device and change there only, in the order of the
+ * stream; every call reads them there, so that a captured graph may be replayed as sequences grow. Host
+ * lens and n_new plan and check the calls; where the two disagree addresses stay inside the buffers.
+ * A step of a server: okvq_q8_extend (all layers at once), then per layer okvq_rotary, okvq_q8_append,
+ * okvq_q8_attention with the granted counts. Calls that change a cache may not overlap other calls on it. */
+enum { OKVQ_Q8_INT8 = 0, OKVQ_Q8_E4M3 = 1 };
+enum { OKVQ_Q8_CROSS = 1u << 0 }; /* okvq_q8_attention: every row sees the whole sequence */
+
+typedef struct {
+  int32_t layers;        /* L, 1..4096                                                    */
+  int32_t batch;         /* B sequence slots, 1..1024                                     */
+  int32_t num_kv_heads;  /* H, 1..4096                                                    */
+  int32_t num_q_heads;   /* Hq, a multiple of H, Hq / H <= 16                             */
+  int32_t head_dim;      /* must be 128                                                   */
+  int32_t num_pages;     /* P, 1..2^20                                                    */
+  int32_t page_tokens;   /* T: 32, 64, 128 or 256                                         */
+  int32_t max_pages;     /* pages of one sequence; max_pages * page_tokens <= 2^27        */
+  int32_t format;        /* OKVQ_Q8_*                                                     */
+  int32_t dtype;         /* OKVQ_F16 or OKVQ_BF16: rows of k, v, q, the stages and out    */
+} okvq_q8_dims;
+
+typedef struct {         /* all device memory, laid out as above, 16-byte aligned */
+  okvq_q8_dims dims;
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* k_scale;
+  float* v_scale;
+  uint16_t* k_stage;
+  uint16_t* v_stage;
+  int32_t* block_table;
+  int32_t* seq_lens;
+  int32_t* page_refs;
+  int32_t* status;
+} okvq_q8_cache;
+
+enum {
+  OKVQ_Q8_BUF_K_CODES = 0, OKVQ_Q8_BUF_V_CODES, OKVQ_Q8_BUF_K_SCALE, OKVQ_Q8_BUF_V_SCALE, OKVQ_Q8_BUF_K_STAGE,
+  OKVQ_Q8_BUF_V_STAGE, OKVQ_Q8_BUF_BLOCK_TABLE, OKVQ_Q8_BUF_SEQ_LENS, OKVQ_Q8_BUF_PAGE_REFS, OKVQ_Q8_BUF_STATUS,
+  OKVQ_Q8_NUM_BUFFERS
+};
+
+/* Bytes of one buffer of the 8-bit cache (0 for an unknown buffer or invalid dims). */
+size_t okvq_q8_buffer_bytes(const okvq_q8_dims* dims, int32_t which_buffer);
+
+/* Quantize the newest tokens of every slot into one layer's pages. okvq_q8_extend has already advanced
+ * the lengths: row i of sequence b is token seq_lens[b] - n_new[b] + i.
+ *   layer       0 .. L - 1
+ *   lens_host   host i32 [B], the lengths with the new tokens, 0 <= lens_host[b] <= max_pages * T
+ *   k_new, v_new  device [B][H][n_max][128]; rows i >= n_new[b] are not read
+ *   n_new_host  host i32 [B], n_new_dev the same on the device, 0 <= n_new <= n_max, n_new <= lens */
+okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* k_new,
+                           const uint16_t* v_new, const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max,
+                           void* stream);
+
+/* Device workspace bytes that okvq_q8_attention needs for sequences up to max_seq_len and up to n_max rows
+ * (0 for invalid arguments). Enough for every shorter call too. No initial contents are needed; calls that
+ * may overlap, captured graphs among them, need one each. */
+size_t okvq_q8_workspace_bytes(const okvq_q8_dims* dims, int32_t max_seq_len, int32_t n_max);
+
+/* Attention of new rows over one layer of the 8-bit cache: one token a sequence (a decode step: the
+ * sequence is split over the GPU), a chunk, or a whole prompt.
+ *   lens_host   host i32 [B]: lengths with the new tokens (plans the launch; the kernels read seq_lens)
+ *   q           device [B][Hq][n_max][128]; query head j reads KV head j / G
+ *   n_new_host, n_new_dev  rows of each sequence, 0 <= n_new <= n_max
+ *   sm_scale    softmax scale, finite
+ *   out         device [B][Hq][n_max][128] of the rows' type; rows i >= n_new[b] are left as they were
+ *   workspace   device, 16-byte aligned, okvq_q8_workspace_bytes(dims, max(lens_host), n_max) bytes
+ *   flags       0: row i sees tokens 0 .. seq_lens[b] - n_new[b] + i (causal). OKVQ_Q8_CROSS: every row
+ *               sees all seq_lens[b] tokens (cross attention to a cache of an encoder's states)
+ * A row that sees no token yields zeros. Codes enter the matrix cores exactly as fp16, softmax statistics
+ * and sums are fp32; the softmax weights times a block's value scale are rounded to fp16. */
+okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                              const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, float sm_scale,
+                              uint16_t* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+
+/* Device workspace bytes of okvq_q8_extend and okvq_q8_compact (0 for invalid dims). No initial contents. */
+size_t okvq_q8_page_workspace_bytes(const okvq_q8_dims* dims);
+
+/* Make room for n_new[b] tokens in every slot and advance seq_lens by them. Pages are taken in the order
+ * of the slots, the lowest free page first. A slot whose last page is partly filled and held by other slots
+ * too gets a copy of it, all layers (copy on write); of the slots that extend a shared page in one call the
+ * last in order keeps the page if no other slot holds it. If there are not enough free pages, or a sequence
+ * would exceed max_pages, nothing changes for any slot and status word 0 is set.
+ *   n_new_dev  device i32 [B] (negative counts as 0)
+ *   granted    device i32 [B] output: n_new, or 0 for every slot if short; pass it on as n_new_dev of
+ *              append and attention. May be n_new_dev itself */
+okvq_status okvq_q8_extend(const okvq_q8_cache* cache, const int32_t* n_new_dev, int32_t* granted, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Make slot dst_host[i] a copy of slot src_host[i], i < n: it shares all pages (nothing is moved) and gets
+ * the raw rows of the open block. What a dst slot held before is freed first.
+ *   src_host, dst_host  host i32 [n], 0 .. B - 1; a slot may be src of several copies, but is dst of one at most
+ *                       and never both (OKVQ_ERR_INVALID_ARGUMENT) */
+okvq_status okvq_q8_fork(const okvq_q8_cache* cache, const int32_t* src_host, const int32_t* dst_host, int32_t n,
+                         void* stream);
+
+/* Empty slots: their pages lose a holder (and are free without one), their table rows become -1, their
+ * lengths 0.  slots_host: host i32 [n], 0 .. B - 1, each at most once. */
+okvq_status okvq_q8_free(const okvq_q8_cache* cache, const int32_t* slots_host, int32_t n, void* stream);
+
+/* Move the pages in use to the front of the pool: with n of them, the k-th page in use at or behind n moves to
+ * the k-th free page before n, in all layers; tables and counts follow. The moved pages' old places keep
+ * their bytes and are free. Status word 1 becomes n. */
+okvq_status okvq_q8_compact(const okvq_q8_cache* cache, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Status words of an 8-bit cache, copied to the host after the work already on `stream` (the call
+ * synchronizes it): status[0] is 1 once an extend was short, status[1] the pages in use after the last
+ * compaction.  status: host i32 [2] */
+okvq_status okvq_q8_status(const okvq_q8_cache* cache, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

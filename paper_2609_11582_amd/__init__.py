@@ -12,3 +12,8 @@ from .okvq import (KVCache, OkvqError, calibration_workspace, decode_workspace, 
                    okvq_dense_workspace_bytes, okvq_cache_status, okvq_prepare_rotation, okvq_quantize_keys,
                    okvq_quantize_keys_mx, okvq_quantize_keys_tq, okvq_quantize_values,
                    okvq_rotation_from_covariance, okvq_value_covariance, okvq_version, status_string)
+from . import q8  # noqa: F401
+from .q8 import (OKVQ_Q8_CROSS, OKVQ_ROTARY_ADJACENT, OKVQ_ROTARY_INVERSE, Q8Cache, make_q8_dims, make_rotary,  # noqa: F401
+                 okvq_q8_append, okvq_q8_attention, okvq_q8_buffer_bytes, okvq_q8_compact, okvq_q8_extend, okvq_q8_fork,
+                 okvq_q8_free, okvq_q8_page_workspace_bytes, okvq_q8_status, okvq_q8_workspace_bytes, okvq_rotary,
+                 q8_page_workspace, q8_workspace)

@@ -1,0 +1,299 @@
+"""Binding of the rotary positions and of the paged 8-bit cache of libokvq.so (include/okvq.h): argument
+marshalling and size checks only, as in ``okvq``. Tensors have to be on the current device and of the stated
+type; the stream is torch's current one unless one is given."""
+
+from __future__ import annotations
+
+import ctypes
+from typing import Sequence
+
+import torch
+
+from .okvq import OkvqError, _check, _i32, _need_len, _stream
+from .okvq import lib as _okvq_lib
+
+OKVQ_F16 = 0
+OKVQ_BF16 = 1
+OKVQ_ROTARY_INVERSE = 1   # the opposite angle: the gradient of the rotation
+OKVQ_ROTARY_ADJACENT = 2  # pairs of channels (2i, 2i + 1) instead of (i, i + 64)
+OKVQ_Q8_INT8 = 0
+OKVQ_Q8_E4M3 = 1
+OKVQ_Q8_CROSS = 1         # every row sees the whole sequence
+Q8_FORMATS = {"int8": OKVQ_Q8_INT8, "e4m3": OKVQ_Q8_E4M3}
+Q8_DTYPES = {"fp16": (OKVQ_F16, torch.float16), "bf16": (OKVQ_BF16, torch.bfloat16)}
+# buffer ids 0..9 of okvq_q8_buffer_bytes (OKVQ_Q8_BUF_*)
+Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_stage", "v_stage", "block_table", "seq_lens", "page_refs",
+              "status")
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64)]
+
+
+class Q8Dims(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("layers", "batch", "num_kv_heads", "num_q_heads", "head_dim", "num_pages",
+                                              "page_tokens", "max_pages", "format", "dtype")]
+
+
+class Q8Struct(ctypes.Structure):
+    _fields_ = [("dims", Q8Dims)] + [(n, ctypes.c_void_p) for n in Q8_BUFFERS]
+
+
+_ready = None
+
+
+def lib() -> ctypes.CDLL:
+    global _ready
+    if _ready is None:
+        L = _okvq_lib()
+        vp, i32, u32, sz, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t, ctypes.POINTER
+        for name, res, args in (
+                ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, P(Rows), P(Rows), vp, P(i32), P(Rows), P(Rows), i32,
+                                      u32, vp]),
+                ("okvq_q8_buffer_bytes", sz, [P(Q8Dims), i32]),
+                ("okvq_q8_append", i32, [P(Q8Struct), i32, P(i32), vp, vp, P(i32), vp, i32, vp]),
+                ("okvq_q8_workspace_bytes", sz, [P(Q8Dims), i32, i32]),
+                ("okvq_q8_attention", i32, [P(Q8Struct), i32, P(i32), vp, P(i32), vp, i32, ctypes.c_float, vp, vp, sz, u32, vp]),
+                ("okvq_q8_page_workspace_bytes", sz, [P(Q8Dims)]),
+                ("okvq_q8_extend", i32, [P(Q8Struct), vp, vp, vp, sz, vp]),
+                ("okvq_q8_fork", i32, [P(Q8Struct), P(i32), P(i32), i32, vp]),
+                ("okvq_q8_free", i32, [P(Q8Struct), P(i32), i32, vp]),
+                ("okvq_q8_compact", i32, [P(Q8Struct), vp, sz, vp]),
+                ("okvq_q8_status", i32, [P(Q8Struct), P(i32), vp])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+        _ready = L
+    return _ready
+
+
+def _need(t: torch.Tensor, nbytes: int, dtype, name: str) -> int:
+    """The tensor's address, once it is contiguous, on the current device, of the type and large enough."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous device tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is {torch.cuda.current_device()}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
+    have = t.numel() * t.element_size()
+    if have < nbytes:
+        raise ValueError(f"{name}: {have} bytes, at least {nbytes} needed")
+    return t.data_ptr()
+
+
+def _workspace(t: torch.Tensor, name: str):
+    return _need(t, 0, None, name), t.numel() * t.element_size()
+
+
+# ---- rotary positions ----------------------------------------------------------------------------
+
+
+def make_rotary(inv_freq: Sequence[float], axes: Sequence[int]) -> RotaryParams:
+    """Frequencies (radians per position) of a row's 64 pairs of channels and the axis (0..2) that turns each."""
+    _need_len(inv_freq, 64, "inv_freq")
+    _need_len(axes, 64, "axes")
+    if any(not 0 <= int(a) <= 2 for a in axes):
+        raise ValueError("axes: 0, 1 or 2 for every pair")
+    return RotaryParams((ctypes.c_double * 64)(*[float(f) for f in inv_freq]), (ctypes.c_uint8 * 64)(*[int(a) for a in axes]))
+
+
+def _rows_of(t: torch.Tensor, batch: int, tokens: int, dtype, name: str) -> Rows:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 4 or t.shape[3] != 128:
+        raise ValueError(f"{name}: expected a device tensor [batch][heads][tokens][128]")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, but the current device is {torch.cuda.current_device()}")
+    if t.shape[0] != batch or t.shape[2] != tokens or t.dtype != dtype:
+        raise ValueError(f"{name}: {list(t.shape)} {t.dtype}, expected batch {batch}, {tokens} tokens, {dtype}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}: the channels of a row have to lie side by side")
+    # the stride of a dimension of one entry is whatever torch left there: it moves nothing
+    s = [t.stride(d) if t.shape[d] > 1 else 0 for d in range(3)]
+    return Rows(t.data_ptr(), s[0], s[1], s[2])
+
+
+def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, flags=0, stream=None, check=True) -> int:
+    """Rotate queries and keys: q, k, q_out, k_out [batch][heads][tokens][128] with any strides over the first
+    three dimensions (``x.view(B, n, heads, 128).transpose(1, 2)`` for a projection's rows), or None in pairs;
+    positions int32 [batch][3][tokens]; lens: rows of each sequence (None: all). In place where an output is its
+    input."""
+    some = q if q is not None else k
+    if not isinstance(some, torch.Tensor) or some.dim() != 4 or some.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("q, k: expected fp16 or bf16 tensors [batch][heads][tokens][128]")
+    B, n, dt = some.shape[0], some.shape[2], some.dtype
+    rows = []
+    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+        if (x is None) != (y is None):
+            raise ValueError(f"{name}: an input and an output, or neither")
+        if x is not None and y.shape != x.shape:
+            raise ValueError(f"{name}_out: {list(y.shape)}, expected {list(x.shape)}")
+        rows.append((None, None) if x is None else (_rows_of(x, B, n, dt, name), _rows_of(y, B, n, dt, name + "_out")))
+    (rq, oq), (rk, ok) = rows
+    pos = _need(positions, B * 3 * n * 4, torch.int32, "positions")
+    if tuple(positions.shape) != (B, 3, n):
+        raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
+    if lens is not None:
+        _need_len(lens, B, "lens")
+    ref = lambda r: None if r is None else ctypes.byref(r)  # noqa: E731
+    st = lib().okvq_rotary(ctypes.byref(rotary), B, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], n, ref(rq),
+                           ref(rk), pos, None if lens is None else _i32(lens), ref(oq), ref(ok),
+                           OKVQ_F16 if dt == torch.float16 else OKVQ_BF16, int(flags), _stream(stream))
+    if check:
+        _check(st, "okvq_rotary")
+    return st
+
+
+# ---- paged 8-bit cache ---------------------------------------------------------------------------
+
+
+def make_q8_dims(batch, num_kv_heads, num_q_heads, num_pages, max_pages, layers=1, page_tokens=64, format="int8",  # noqa: A002
+                 dtype="fp16", head_dim=128) -> Q8Dims:
+    return Q8Dims(layers, batch, num_kv_heads, num_q_heads, head_dim, num_pages, page_tokens, max_pages, Q8_FORMATS[format],
+                  Q8_DTYPES[dtype][0])
+
+
+def okvq_q8_buffer_bytes(dims: Q8Dims, which: int) -> int:
+    return lib().okvq_q8_buffer_bytes(ctypes.byref(dims), which)
+
+
+class Q8Cache:
+    """The paged 8-bit cache of `layers` layers: device buffers sized by okvq_q8_buffer_bytes (torch allocations,
+    a new cache's contents), or the caller's (`buffers`, by name, taken as they are).
+    format "int8" or "e4m3"; dtype "fp16" or "bf16": the rows of keys, values, queries and outputs."""
+
+    def __init__(self, batch, num_kv_heads, num_q_heads, num_pages, max_pages, layers=1, page_tokens=64,
+                 format="int8", dtype="fp16", device="cuda", buffers=None):  # noqa: A002
+        self.dims = make_q8_dims(batch, num_kv_heads, num_q_heads, num_pages, max_pages, layers, page_tokens, format, dtype)
+        self.format, self.row_dtype = format, Q8_DTYPES[dtype][1]
+        types = dict(k_codes=torch.uint8, v_codes=torch.uint8, k_scale=torch.float32, v_scale=torch.float32,
+                     k_stage=self.row_dtype, v_stage=self.row_dtype)
+        L, B, H, P, T, W = layers, batch, num_kv_heads, num_pages, page_tokens, 32
+        shapes = dict(k_codes=(L, P, H, T, 128), v_codes=(L, P, H, T // W, 128 * W), k_scale=(L, P, H, T // W),
+                      v_scale=(L, P, H, T // W), k_stage=(L, B, H, W, 128), v_stage=(L, B, H, W, 128),
+                      block_table=(B, max_pages), seq_lens=(B,), page_refs=(P,), status=(4,))
+        self.buffers = {}
+        for i, name in enumerate(Q8_BUFFERS):
+            dt = types.get(name, torch.int32)
+            nbytes = okvq_q8_buffer_bytes(self.dims, i)
+            if nbytes == 0:
+                raise OkvqError(-1, f"okvq_q8_buffer_bytes({name})")
+            if buffers is not None:
+                t = buffers[name]
+                _need(t, nbytes, dt, name)
+            else:
+                t = torch.full(shapes[name], -1 if name == "block_table" else 0, dtype=dt, device=device)
+            self.buffers[name] = t
+        self.struct = Q8Struct(self.dims, *[self.buffers[n].data_ptr() for n in Q8_BUFFERS])
+        self.device_index = self.buffers["k_codes"].get_device()
+
+    def __getitem__(self, name):
+        return self.buffers[name]
+
+
+def _cache_ref(cache: Q8Cache):
+    if cache.device_index != torch.cuda.current_device():
+        raise ValueError(f"cache: on device {cache.device_index}, but the current device is {torch.cuda.current_device()}")
+    return ctypes.byref(cache.struct)
+
+
+def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, n_max, stream=None, check=True) -> int:
+    """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128]) into one layer's pages, after
+    okvq_q8_extend; lens: the lengths with them."""
+    d = cache.dims
+    ref = _cache_ref(cache)
+    _need_len(lens, d.batch, "lens")
+    _need_len(n_new, d.batch, "n_new")
+    nbytes = d.batch * d.num_kv_heads * int(n_max) * 256
+    st = lib().okvq_q8_append(ref, int(layer), _i32(lens), _need(k_new, nbytes, cache.row_dtype, "k_new"),
+                              _need(v_new, nbytes, cache.row_dtype, "v_new"), _i32(n_new),
+                              _need(n_new_dev, d.batch * 4, torch.int32, "n_new_dev"), int(n_max), _stream(stream))
+    if check:
+        _check(st, "okvq_q8_append")
+    return st
+
+
+def okvq_q8_workspace_bytes(dims: Q8Dims, max_seq_len: int, n_max: int = 1) -> int:
+    return lib().okvq_q8_workspace_bytes(ctypes.byref(dims), int(max_seq_len), int(n_max))
+
+
+def q8_workspace(dims: Q8Dims, max_seq_len: int, n_max: int = 1, device="cuda") -> torch.Tensor:
+    """A workspace of okvq_q8_workspace_bytes bytes for okvq_q8_attention (no contents needed)."""
+    return torch.empty(max(okvq_q8_workspace_bytes(dims, max_seq_len, n_max) + 15, 16) // 16 * 4, dtype=torch.float32,
+                       device=device)
+
+
+def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, sm_scale, out, workspace, flags=0,
+                      stream=None, check=True) -> int:
+    """Attention of rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
+    tokens of each sequence, causal, or OKVQ_Q8_CROSS. lens: the lengths with the new tokens."""
+    d = cache.dims
+    ref = _cache_ref(cache)
+    _need_len(lens, d.batch, "lens")
+    _need_len(n_new, d.batch, "n_new")
+    nbytes = d.batch * d.num_q_heads * int(n_max) * 256
+    ws, ws_bytes = _workspace(workspace, "workspace")
+    st = lib().okvq_q8_attention(ref, int(layer), _i32(lens), _need(q, nbytes, cache.row_dtype, "q"), _i32(n_new),
+                                 _need(n_new_dev, d.batch * 4, torch.int32, "n_new_dev"), int(n_max), float(sm_scale),
+                                 _need(out, nbytes, cache.row_dtype, "out"), ws, ws_bytes, int(flags), _stream(stream))
+    if check:
+        _check(st, "okvq_q8_attention")
+    return st
+
+
+def okvq_q8_page_workspace_bytes(dims: Q8Dims) -> int:
+    return lib().okvq_q8_page_workspace_bytes(ctypes.byref(dims))
+
+
+def q8_page_workspace(dims: Q8Dims, device="cuda") -> torch.Tensor:
+    """A workspace of okvq_q8_page_workspace_bytes bytes for okvq_q8_extend and okvq_q8_compact (no contents needed)."""
+    return torch.empty(max(okvq_q8_page_workspace_bytes(dims) + 15, 16) // 16 * 4, dtype=torch.int32, device=device)
+
+
+def okvq_q8_extend(cache: Q8Cache, n_new_dev, granted, workspace, stream=None, check=True) -> int:
+    """Pages for n_new_dev[b] more tokens in every slot and the lengths advanced by them; granted (int32 [B], device):
+    the same counts, or 0 for all where pages are short."""
+    B = cache.dims.batch
+    ref = _cache_ref(cache)
+    ws, ws_bytes = _workspace(workspace, "workspace")
+    st = lib().okvq_q8_extend(ref, _need(n_new_dev, B * 4, torch.int32, "n_new_dev"),
+                              _need(granted, B * 4, torch.int32, "granted"), ws, ws_bytes, _stream(stream))
+    if check:
+        _check(st, "okvq_q8_extend")
+    return st
+
+
+def okvq_q8_fork(cache: Q8Cache, src, dst, stream=None, check=True) -> int:
+    """Slot dst[i] becomes a copy of slot src[i] that shares its pages."""
+    _need_len(dst, len(src), "dst")
+    st = lib().okvq_q8_fork(_cache_ref(cache), _i32(src), _i32(dst), len(src), _stream(stream))
+    if check:
+        _check(st, "okvq_q8_fork")
+    return st
+
+
+def okvq_q8_free(cache: Q8Cache, slots, stream=None, check=True) -> int:
+    """Empty slots; pages without another holder are free."""
+    st = lib().okvq_q8_free(_cache_ref(cache), _i32(slots), len(slots), _stream(stream))
+    if check:
+        _check(st, "okvq_q8_free")
+    return st
+
+
+def okvq_q8_compact(cache: Q8Cache, workspace, stream=None, check=True) -> int:
+    """Move the pages in use to the front of the pool."""
+    ref = _cache_ref(cache)
+    ws, ws_bytes = _workspace(workspace, "workspace")
+    st = lib().okvq_q8_compact(ref, ws, ws_bytes, _stream(stream))
+    if check:
+        _check(st, "okvq_q8_compact")
+    return st
+
+
+def okvq_q8_status(cache: Q8Cache, stream=None):
+    """(1 once an extend was short of pages, pages in use after the last compaction). Synchronizes `stream`."""
+    words = (ctypes.c_int32 * 2)()
+    _check(lib().okvq_q8_status(_cache_ref(cache), words, _stream(stream)), "okvq_q8_status")
+    return int(words[0]), int(words[1])

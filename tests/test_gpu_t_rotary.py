@@ -1,0 +1,184 @@
+"""Rotary positions on several axes against the float64 rotation (oracle.q8.rotate): both pairings, the gradient, types,
+layouts, in place, ragged batches whose other rows stay untouched, far and negative positions.
+
+Tolerance per element, of a pair (a, b) of inputs: the output's rounding, half a step of its type relative to the
+result (fp16 2^-11, bf16 2^-8; 2^-25 absolute for fp16's subnormals), and (|a| + |b|) 2^-21 for the angle's fraction
+of a turn (2^-25 of a half turn, times pi), sine, cosine (2^-23 each) and the two fp32 products."""
+
+import numpy as np
+import pytest
+
+from oracle import q8 as oq
+
+pytestmark = pytest.mark.gpu
+FREQ = [1e6 ** (-i / 64) for i in range(64)]
+AXES = [0] * 16 + [1] * 24 + [2] * 24
+HALF = {"fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def _t(dtype):
+    import torch
+    return torch.float16 if dtype == "fp16" else torch.bfloat16
+
+
+def _inputs(B, heads, n, dtype, seed, far=False):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(B, n, heads, 128, generator=g).to(_t(dtype))
+    lo, hi = (-(1 << 31), (1 << 31) - 1) if far else (0, 140000)
+    pos = torch.randint(lo, hi, (B, 3, n), generator=g).to(torch.int32)
+    return x, pos
+
+
+def _check(got, x, pos, dtype, tag, **kw):
+    ref = oq.rotate(x, pos, FREQ, AXES, **kw)
+    a, b = (slice(0, 128, 2), slice(1, 128, 2)) if kw.get("adjacent") else (slice(0, 64), slice(64, 128))
+    size = np.empty_like(ref)
+    size[..., a] = size[..., b] = np.abs(x[..., a]) + np.abs(x[..., b])
+    err = np.abs(got - ref) / (HALF[dtype] * np.abs(ref) + 2.0 ** -21 * size + 2.0 ** -25)
+    print(f"[gpu-case] {tag}: worst err / tolerance {err.max():.3f}", flush=True)
+    assert err.max() <= 1
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("B, hq, hk, n", [(1, 28, 4, 1), (3, 7, 1, 37), (1, 1, 1, 8), (2, 16, 2, 9)])
+def test_rotation(dtype, inverse, adjacent, B, hq, hk, n):
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    q, pos = _inputs(B, hq, n, dtype, 1)
+    k, _ = _inputs(B, hk, n, dtype, 2)
+    flags = (okvq.OKVQ_ROTARY_INVERSE if inverse else 0) | (okvq.OKVQ_ROTARY_ADJACENT if adjacent else 0)
+    qd, kd = q.cuda().transpose(1, 2), k.cuda().transpose(1, 2)  # token by token in memory
+    qo, ko = torch.empty(B, hq, n, 128, dtype=q.dtype, device="cuda"), torch.empty(B, hk, n, 128, dtype=q.dtype, device="cuda")
+    okvq.okvq_rotary(okvq.make_rotary(FREQ, AXES), qd, kd, pos.cuda(), qo, ko, flags=flags)
+    for x, y in ((q, qo), (k, ko)):
+        _check(y.double().cpu().numpy(), x.transpose(1, 2).double().numpy(), pos.numpy(), dtype, f"{B}x{hq}x{n} {dtype}",
+               inverse=inverse, adjacent=adjacent)
+
+
+def test_far_positions_and_axes():
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    x, pos = _inputs(2, 3, 21, "fp16", 3, far=True)
+    pos[0, :, :4] = torch.tensor([0, -1, (1 << 31) - 1, -(1 << 31)])
+    axes = [(5 * i) % 3 for i in range(64)]  # interleaved axes
+    freq = [0.0, 1.0, 3.0, -0.7] + [1e4 ** (-i / 64) for i in range(4, 64)]  # none, more than one turn's worth, backwards
+    d = x.cuda().transpose(1, 2)
+    out = torch.empty_like(d)
+    okvq.okvq_rotary(okvq.make_rotary(freq, axes), None, d, pos.cuda(), None, out)
+    # the oracle's angle in turns, modulo one, in extended precision: at 2^31 radians a double is 2^-22 off
+    t = np.array(freq, np.longdouble) / (2 * np.longdouble(np.pi) + np.longdouble(2 * 1.2246467991473532e-16))
+    turns = pos.numpy()[:, axes, :].astype(np.longdouble).transpose(0, 2, 1)[:, None] * t
+    # the frequency itself is a double: its 2^-53 is worth 2^-22 of a radian at position 2^31
+    angle = ((turns - np.rint(turns)) * 2 * np.longdouble(np.pi)).astype(np.float64)
+    xs = x.transpose(1, 2).double().numpy()
+    c, s = np.cos(angle), np.sin(angle)
+    ref = np.concatenate([xs[..., :64] * c - xs[..., 64:] * s, xs[..., 64:] * c + xs[..., :64] * s], -1)
+    size = np.abs(xs[..., :64]) + np.abs(xs[..., 64:])
+    size = np.concatenate([size, size], -1)
+    # 2^-20 more than elsewhere: turn[i] holds the frequency to a double's 2^-53, 2^31 * 3 rad * 2^-53 < 2^-20
+    err = np.abs(out.double().cpu().numpy() - ref) / (HALF["fp16"] * np.abs(ref) + 2.0 ** -19 * size + 2.0 ** -25)
+    print(f"[gpu-case] far positions: worst err / tolerance {err.max():.3f}", flush=True)
+    assert err.max() <= 1
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_ragged_rows_and_layouts(dtype):
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B, H, n = 5, 3, 19
+    lens = [19, 0, 1, 8, 17]
+    x, pos = _inputs(B, H, n, dtype, 4)
+    for b, m in enumerate(lens):
+        x[b, m:] = float("nan")
+    par = okvq.make_rotary(FREQ, AXES)
+    # one fused projection's rows [B][n][H + 2][128], a slice of its heads
+    wide = torch.full((B, n, H + 2, 128), 7.0, dtype=x.dtype, device="cuda")
+    wide[:, :, 1:1 + H] = x.cuda()
+    src = wide[:, :, 1:1 + H].transpose(1, 2)
+    out = torch.full((B, n, H, 128), 5.0, dtype=x.dtype, device="cuda")
+    okvq.okvq_rotary(par, src, None, pos.cuda(), out.transpose(1, 2), None, lens=lens)
+    same = src.contiguous()
+    okvq.okvq_rotary(par, same, None, pos.cuda(), same, None, lens=lens)  # in place
+    wide2 = wide.clone()
+    inside = wide2[:, :, 1:1 + H].transpose(1, 2)
+    okvq.okvq_rotary(par, inside, None, pos.cuda(), inside, None, lens=lens)  # in place, strided
+    assert bool((wide2[:, :, 0] == 7).all()) and bool((wide2[:, :, 1 + H:] == 7).all())
+    for b, m in enumerate(lens):
+        assert bool((out[b, m:] == 5).all()) and bool(same[b, :, m:].isnan().all())
+        if m:
+            got = out[b, :m].transpose(0, 1)
+            assert torch.equal(got, same[b, :, :m]) and torch.equal(got, inside[b, :, :m])
+            _check(got.double().cpu().numpy()[None], x[b, :m].transpose(0, 1).double().numpy()[None], pos.numpy()[b:b + 1, :, :m], dtype,
+                   f"sequence {b}")
+
+
+def test_many_sequences():
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B = 515  # three launches of up to 256
+    x, pos = _inputs(B, 2, 3, "fp16", 6)
+    lens = [b % 4 for b in range(B)]
+    d = x.cuda().transpose(1, 2)
+    out = torch.zeros(B, 2, 3, 128, dtype=torch.float16, device="cuda")
+    okvq.okvq_rotary(okvq.make_rotary(FREQ, AXES), None, d, pos.cuda(), None, out, lens=lens)
+    ref = oq.rotate(x.transpose(1, 2).double().numpy(), pos.numpy(), FREQ, AXES)
+    live = (np.arange(3) < np.array(lens)[:, None])[:, None, :, None]
+    got = out.double().cpu().numpy()
+    assert np.all(np.where(live, 0, got) == 0)
+    assert np.abs(np.where(live, got - ref, 0)).max() <= 2.0 ** -11 * 6 + 2.0 ** -18
+
+
+def test_gradient_against_differences_of_the_loss():
+    """loss = sum g * rotate(x): linear in x, so differences of any step are exact up to rounding; step 1 along random
+    directions against <direction, gradient>."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B, H, n = 1, 2, 40
+    g = torch.Generator().manual_seed(8)
+    x, up, way = (torch.randn(B, H, n, 128, generator=g) for _ in range(3))
+    pos = torch.randint(0, 5000, (B, 3, n), generator=g).to(torch.int32).cuda()
+    par = okvq.make_rotary(FREQ, AXES)
+
+    def turn(v, flags=0):
+        d = v.to(torch.bfloat16).cuda()
+        out = torch.empty_like(d)
+        okvq.okvq_rotary(par, d, None, pos, out, None, flags=flags)
+        return out.double().cpu()
+    x, up, way = (v.to(torch.bfloat16).float() for v in (x, up, way))
+    moved = (x + way).to(torch.bfloat16).float()
+    way = moved - x  # what the step is after rounding
+    change = float((up.double() * (turn(moved) - turn(x))).sum())
+    grad = turn(up, okvq.OKVQ_ROTARY_INVERSE)
+    # three rounded results of unit size, 2^-8 each at most: random signs over 10240 terms, 6 sigma
+    assert abs(change - float((way.double() * grad).sum())) <= 6 * 2.0 ** -8 * 3 * (B * H * n * 128) ** 0.5
+
+
+def test_refuses_wrong_tensors():
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    par = okvq.make_rotary(FREQ, AXES)
+    x = torch.zeros(1, 2, 4, 128, dtype=torch.float16, device="cuda")
+    pos = torch.zeros(1, 3, 4, dtype=torch.int32, device="cuda")
+    for bad in (x.float(), x[..., :64], x[:, :, :3], torch.zeros(1, 2, 4, 256, dtype=torch.float16, device="cuda")[..., ::2]):
+        with pytest.raises(ValueError):
+            okvq.okvq_rotary(par, bad, None, pos, bad, None)
+    with pytest.raises(ValueError):
+        okvq.okvq_rotary(par, x, None, pos, x.bfloat16(), None)
+    with pytest.raises(ValueError):
+        okvq.okvq_rotary(par, x, None, pos, x.cpu(), None)
+    with pytest.raises(ValueError):
+        okvq.okvq_rotary(par, x, None, pos.long(), x, None)
+    with pytest.raises(ValueError):
+        okvq.okvq_rotary(par, x, x, pos, x, None)
+    odd = torch.zeros(1, 2, 4, 132, dtype=torch.float16, device="cuda")[..., :128]  # rows 264 bytes apart
+    with pytest.raises(okvq.OkvqError):
+        okvq.okvq_rotary(par, odd, None, pos, x, None)
