@@ -14,7 +14,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libokvq.so")
 SOURCES = ["api.hip", "codec_kernels.hip", "codec_fused.hip", "decode_kernels.hip", "calib_kernels.hip",
            "dense_decode.hip", "ladder_codec.hip", "ladder_decode.hip", "append_window.hip", "codec_block.hip",
-           "rotary.hip", "q8_api.hip", "q8_append.hip", "q8_attention.hip", "q8_pages.hip"]
+           "rotary.hip", "q8_api.hip", "q8_append.hip", "q8_attention.hip", "q8_prompt.hip",
+           "q8_pages.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

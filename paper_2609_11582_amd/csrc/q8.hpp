@@ -10,6 +10,7 @@ namespace okvq {
 constexpr int kQ8Block = kW * kD;  // bytes of one block of codes: 32 tokens x 128 channels
 constexpr int kQ8MaxBatch = 1024;  // slots: one thread each in the page kernels
 constexpr int kQ8Cols = 16;        // query columns of a tile of the split kernel
+constexpr int kQ8PromptCols = 256; // and of the prompt kernel
 
 // ---- rotary --------------------------------------------------------------------------------------
 struct RotaryArgs {
@@ -63,6 +64,7 @@ struct Q8Plan {
 Q8Plan q8_plan(int B, int H, int G, int n_max, int max_len);
 size_t q8_plan_bytes(const Q8Plan& p, int B, int H);           // split records of a call
 size_t q8_workspace_bound(int B, int H, int G, int n_max, int max_len);  // of every call up to these sizes
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, int format, int dtype, int B, hipStream_t s);
 hipError_t launch_q8_attention(Q8AttendArgs a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
 
 // Page calls, on the whole cache

@@ -119,7 +119,10 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[tb][e]);
     mx = max32(max16(mx));
-    const float lv = __builtin_amdgcn_logf(x.vs);
+    float lv = __builtin_amdgcn_logf(x.vs);
+    // a block whose values are all zero has scale 1: it adds to the sum alone and must not move M (a subnormal
+    // scale has lv = -inf here, and the same)
+    if (x.vs == 1.0f && !__any(((or4(x.v[0]) | or4(x.v[1]) | or4(x.v[2]) | or4(x.v[3])) & 0x7f7f7f7fu) != 0)) lv = -__builtin_inff();
     if (__any(mx > m + kLazy || mx + lv > M + kLazy)) {
       const float m2 = fmaxf(m, mx), M2 = fmaxf(M, mx + lv);
       l *= __builtin_amdgcn_exp2f(m - m2);
@@ -252,11 +255,19 @@ __global__ __launch_bounds__(256) void k_q8_merge(Q8AttendArgs p, int cols) {
 
 Q8Plan q8_plan(int B, int H, int G, int n_max, int max_len) {
   Q8Plan p;
-  p.cols = kQ8Cols;
-  p.ntile = (int)(((int64_t)n_max * G + p.cols - 1) / p.cols);
-  const int64_t units = (int64_t)B * H * p.ntile, blocks = (max_len + kW - 1) / kW;
-  // work-groups for every compute unit; a split has at least a block for each wave
-  const int64_t want = (kQ8Groups + units - 1) / units, most = (blocks + kWaves - 1) / kWaves;
+  const int64_t rows = (int64_t)n_max * G;
+  p.cols = rows <= kQ8Cols ? kQ8Cols : kQ8PromptCols;
+  p.ntile = (int)((rows + p.cols - 1) / p.cols);
+  const int64_t units = (int64_t)B * H * p.ntile;
+  int64_t want, most;
+  if (p.cols == kQ8Cols) {
+    // work-groups for every compute unit; a split has at least a block for each wave
+    want = (kQ8Groups + units - 1) / units;
+    most = ((max_len + kW - 1) / kW + kWaves - 1) / kWaves;
+  } else {
+    want = (kQ8PromptGroups + units - 1) / units;
+    most = (max_len + kQ8PromptSplit - 1) / kQ8PromptSplit;
+  }
   p.nsplit = (int)std::max<int64_t>(1, std::min({want, most, (int64_t)kQ8MaxSplits}));
   return p;
 }
@@ -266,11 +277,19 @@ size_t q8_plan_bytes(const Q8Plan& p, int B, int H) {
   return (size_t)B * H * p.ntile * p.nsplit * p.cols * (kD + 4) * sizeof(float);
 }
 
-// Shorter calls and calls of fewer rows have up to kQ8Groups + their units records
+// A call of u units (tiles of every sequence and head) has at most the groups it is split into and u records more;
+// calls of fewer rows have no more units of the same kind, and a call of few rows has B H
 size_t q8_workspace_bound(int B, int H, int G, int n_max, int max_len) {
-  const Q8Plan p = q8_plan(B, H, G, n_max, max_len);
-  const size_t units = (size_t)B * H * p.ntile;
-  return (units + kQ8Groups) * p.cols * (kD + 4) * sizeof(float);
+  const size_t few = ((size_t)B * H + kQ8Groups) * kQ8Cols;
+  const int64_t rows = (int64_t)n_max * G;
+  size_t many = 0;
+  if (rows > kQ8Cols) {
+    const size_t units = (size_t)B * H * ((rows + kQ8PromptCols - 1) / kQ8PromptCols);
+    many = std::min(units, (size_t)kQ8PromptGroups) + kQ8PromptGroups;  // units of kQ8PromptGroups and more are not split
+    many *= kQ8PromptCols;
+  }
+  (void)max_len;
+  return std::max(few, many) * (kD + 4) * sizeof(float);
 }
 
 hipError_t launch_q8_attention(Q8AttendArgs a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
@@ -278,14 +297,17 @@ hipError_t launch_q8_attention(Q8AttendArgs a, const Q8Plan& p, int format, int 
   a.ntile = p.ntile;
   const dim3 grid(p.nsplit, a.c.H * p.ntile, B), block(kThreads);
   const bool bf16 = dtype == OKVQ_BF16;
-  if (format == OKVQ_Q8_INT8) {
+  hipError_t e;
+  if (p.cols == kQ8PromptCols) {
+    e = launch_q8_prompt(a, format, dtype, B, s);
+  } else if (format == OKVQ_Q8_INT8) {
     if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
   } else {
     if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, false>), grid, block, 0, s, a);
   }
-  hipError_t e = hipGetLastError();
+  if (p.cols == kQ8Cols) e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const dim3 mgrid(p.cols, a.c.H * p.ntile, B);
   if (bf16) hipLaunchKernelGGL((k_q8_merge<true>), mgrid, dim3(256), 0, s, a, p.cols);

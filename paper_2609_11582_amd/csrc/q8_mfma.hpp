@@ -15,12 +15,16 @@ constexpr float kNoScore = -1e30f;   // a reference before any token; finite, so
 constexpr float kLazy = 8.0f;        // references move when passed by 2^8
 constexpr float kWeightExp = 7.0f;   // weights are at most 2^(kLazy + kWeightExp)
 constexpr int kQ8MaxSplits = 128;
-constexpr int kQ8Groups = 512;       // work-groups a call is split into
+constexpr int kQ8Groups = 512;       // work-groups that a call of few rows is split into
+constexpr int kQ8PromptGroups = 256; // and a call of many: one for each compute unit
+constexpr int kQ8PromptSplit = 512;  // least tokens of a split of the prompt kernel
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const half2v v = {(_Float16)lo, (_Float16)hi};
   return __builtin_bit_cast(uint32_t, v);
 }
+
+__device__ __forceinline__ uint32_t or4(uint4 v) { return v.x | v.y | v.z | v.w; }
 
 // Two of a dword's codes as fp16, exactly. int8: byte code ^ 0x80 under the exponent of 1024 is 1024 + 128 + code.
 template <int kFmt, bool kHigh>

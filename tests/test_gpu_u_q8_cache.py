@@ -583,3 +583,31 @@ def test_binding_refuses():
         okvq.Q8Cache(1, 1, 1, 4, 2, buffers={f: t.cpu() for f, t in okvq.Q8Cache(1, 1, 1, 4, 2).buffers.items()})
     with pytest.raises(okvq.OkvqError):
         okvq.Q8Cache(1, 1, 17, 4, 2)
+
+
+@pytest.mark.parametrize("n_q", [1, 40])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_blocks_of_zero_values(fmt, n_q):
+    """Blocks of zero values (scale 1) that take most of the attention, among blocks of tiny values."""
+    import torch
+    n = 1000
+    c = _new(1, 1, 2, [n], 64, fmt)
+    g = torch.Generator().manual_seed(7)
+    k, v = 0.1 * torch.randn(1, 1, n, 128, generator=g), 1e-4 * torch.randn(1, 1, n, 128, generator=g)
+    k[0, 0, 32:64, 0] += 8.0
+    v[0, 0, 32:64] = 0.0
+    v[0, 0, 320:352] = -0.0
+    k, v = k.half(), v.half()
+    _append(c, 0, k, v, [0], [n])
+    q = torch.zeros(1, 2, n_q, 128)
+    q[:, :, :, 0] = math.log(2.0) / SM
+    q[:, 1] = 0.0
+    q = q.half()
+    out = _attend(c, [n], q, [n_q])
+    a = _numpy(c)
+    kk, vv = oq.read_sequence(a, 0, 0, 0, n, fmt)
+    for j in range(2):
+        ref, bound = oq.attention(q[0, j].double().numpy(), kk, vv, n - n_q + np.arange(n_q) + 1, SM, HALF["fp16"])
+        r = np.abs(out[0, j].double().cpu().numpy() - ref) / bound
+        _say(f"zero blocks {fmt} rows {n_q} head {j}: worst err / bound {r.max():.3f}")
+        assert r.max() <= 1
