@@ -48,24 +48,32 @@ struct Q8AppendArgs {
 };
 hipError_t launch_q8_append(const Q8AppendArgs& a, int format, int dtype, int B, int blocks, hipStream_t s);
 
+// Splits of each sequence: sequence b has those from first[b] on, up to first[b + 1]; with none there it has one split,
+// which writes the output rows itself
+struct Q8Splits {
+  uint16_t first[kQ8MaxBatch + 1];
+};
 struct Q8AttendArgs {
   Q8View c;
   const uint16_t* q;
   const int32_t* n_new;
   uint16_t* out;
   float* ws;
-  int n_max, G, nsplit, ntile, cross;
+  int n_max, G, ntile, cross;
   float qscale;  // sm_scale log2(e)
+  Q8Splits splits;
 };
 struct Q8Plan {
   int cols;    // query columns of a tile: rows of a KV head's group, G to a position
-  int ntile, nsplit;
+  int ntile;
+  int rows;    // columns that rows have in the first tile
+  int most;    // splits of the sequence that has most
+  Q8Splits splits;
 };
-Q8Plan q8_plan(int B, int H, int G, int n_max, int max_len);
-size_t q8_plan_bytes(const Q8Plan& p, int B, int H);           // split records of a call
-size_t q8_workspace_bound(int B, int H, int G, int n_max, int max_len);  // of every call up to these sizes
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, int format, int dtype, int B, hipStream_t s);
-hipError_t launch_q8_attention(Q8AttendArgs a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
+void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens);
+size_t q8_workspace_bound(int G, int n_max);  // split records of every call of up to n_max rows
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, int most, int format, int dtype, int B, hipStream_t s);
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
 
 // Page calls, on the whole cache
 struct Q8Pages {
@@ -119,9 +127,15 @@ __device__ __forceinline__ uint32_t row_pack(float lo, float hi) {
   return row_bits<kBf16>(lo) | (row_bits<kBf16>(hi) << 16);
 }
 
-// Page of a block of a sequence, inside the pool whatever the table holds
+// A load from a wave-uniform address through the scalar cache: for what earlier launches wrote and this one only
+// reads. As a vector load, the wait for it would wait for every load in flight before it
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+// Page of a block of a sequence, inside the pool whatever the table holds; the block is wave-uniform
 __device__ __forceinline__ int q8_page(const int32_t* row, int block, const Q8View& c) {
-  const int id = row[min(block >> c.bshift, c.max_pages - 1)];
+  const int id = uniform_load(row + min(block >> c.bshift, c.max_pages - 1));
   return min(max(id, 0), c.P - 1);
 }
 // Index of (page, head, block within the page) among the blocks of a layer
@@ -129,7 +143,7 @@ __device__ __forceinline__ int64_t q8_slot(int page, int h, int block, const Q8V
   return (((int64_t)page * c.H + h) << c.bshift) + (block & ((1 << c.bshift) - 1));
 }
 __device__ __forceinline__ int q8_len(const Q8View& c, int b) {
-  return min(max(c.lens[b], 0), c.max_pages << (c.bshift + 5));
+  return min(max(uniform_load(c.lens + b), 0), c.max_pages << (c.bshift + 5));
 }
 
 }  // namespace okvq

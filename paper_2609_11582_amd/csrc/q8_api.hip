@@ -123,14 +123,15 @@ okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t
   if ((int64_t)hq + hk > 65535) return OKVQ_ERR_UNSUPPORTED;
   for (const okvq_rows* r : {q, k, q_out, k_out})
     if (r && check_rows_of(r) != OKVQ_OK) return OKVQ_ERR_INVALID_ARGUMENT;
-  RotaryArgs a{};
+  RotaryArgs a;
+  a.q = a.k = a.q_out = a.k_out = okvq_rows{};
   for (int i = 0; i < 64; ++i) {
     if (params->axis[i] > 2 || !std::isfinite(params->inv_freq[i])) return OKVQ_ERR_INVALID_ARGUMENT;
     a.axis[i] = params->axis[i];
     // turns per position, modulo one (positions are whole numbers), in units of 2^-64
     double t = params->inv_freq[i] / (2.0 * M_PI);
     t -= std::floor(t);
-    const double scaled = std::ldexp(t, 64);
+    const double scaled = t * 0x1p64;
     a.turn[i] = scaled < 0x1p64 ? (uint64_t)scaled : 0;
   }
   if (q) {
@@ -202,7 +203,7 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
 
 size_t okvq_q8_workspace_bytes(const okvq_q8_dims* d, int32_t max_seq_len, int32_t n_max) {
   if (check_dims(d) != OKVQ_OK || max_seq_len < 0 || n_max < 1) return 0;
-  return q8_workspace_bound(d->batch, d->num_kv_heads, d->num_q_heads / d->num_kv_heads, n_max, max_seq_len);
+  return q8_workspace_bound(d->num_q_heads / d->num_kv_heads, n_max);
 }
 
 okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
@@ -220,12 +221,14 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
   if (st != OKVQ_OK) return st;
   if (most == 0) return OKVQ_OK;
   const int G = d.num_q_heads / d.num_kv_heads;
-  const Q8Plan plan = q8_plan(d.batch, d.num_kv_heads, G, most, max_len);
-  if (!aligned16(workspace) || workspace_bytes < q8_plan_bytes(plan, d.batch, d.num_kv_heads)) return OKVQ_ERR_WORKSPACE;
-  if (!launchable((int64_t)plan.nsplit * plan.ntile * d.num_kv_heads * d.batch, 512) ||
-      (int64_t)plan.ntile * d.num_kv_heads > INT32_MAX)
+  Q8Plan plan;
+  q8_plan(plan, d.batch, d.num_kv_heads, G, most, lens_host);
+  if (!aligned16(workspace) || workspace_bytes < q8_workspace_bound(G, most)) return OKVQ_ERR_WORKSPACE;
+  if (!launchable((int64_t)plan.most * plan.ntile * d.num_kv_heads * d.batch, 512) ||
+      (plan.most > 1 && (!launchable((int64_t)plan.ntile * d.num_kv_heads * d.batch * 32, 256) ||
+                         (int64_t)plan.ntile * d.num_kv_heads > 65535)))
     return OKVQ_ERR_UNSUPPORTED;
-  Q8AttendArgs a{};
+  Q8AttendArgs a;
   a.c = view(cache, layer);
   a.q = q;
   a.n_new = n_new_dev;

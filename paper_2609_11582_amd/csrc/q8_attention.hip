@@ -31,55 +31,67 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRecFloatsQ8 = kQ8Cols * (kD + 4);  // a split's record: [16][128] sums, then [16] of (M, m, l, 0)
 constexpr int kCombineRow = kD + 4;               // floats of a combine row: 16 rows of a column fall into all banks
 
-struct BlockRegs {
-  uint4 k[2][2];  // key rows 16 tb + col: channels 16 g .. + 15 and 64 + 16 g .. + 15
-  uint4 v[4];     // value slots 64 j + lane
-  float ks, vs;
-};
-
 template <int kFmt, bool kBf16>
-__global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
+__global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __shared__ __attribute__((aligned(16))) float cmb[kWaves][kQ8Cols * kCombineRow];
   __shared__ float wM[kWaves][kQ8Cols], wm[kWaves][kQ8Cols], wl[kWaves][kQ8Cols];
   const Q8View& c = p.c;
-  const int split = blockIdx.x, h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
+  const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int first = p.splits.first[b], records = p.splits.first[b + 1] - first, nsplit = max(records, 1);
+  if (split >= nsplit) return;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* row = c.table + (int64_t)b * c.max_pages;
-  const int len = q8_len(c, b), n = min(max(p.n_new[b], 0), p.n_max);
-  const int r0 = tile * kQ8Cols, i_first = r0 / p.G;
-  if (i_first >= n) return;  // no live row in the tile
-  const int i_last = min((r0 + kQ8Cols - 1) / p.G, n - 1);
-  const int vis_first = p.cross ? len : max(len - n + i_first + 1, 0);  // tokens that the tile's first and last rows see
-  const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
-  const int i = (r0 + col) / p.G, hq = h * p.G + (r0 + col - i * p.G);
-  const bool live = i < n;
-  const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
-  const int nblk = (vis_last + kW - 1) / kW, stride = p.nsplit * kWaves;
+  const int stride = nsplit * kWaves;
+  int block = split * kWaves + wave;
 
-  auto load = [&](int block, BlockRegs& x) {
-    const int64_t slot = q8_slot(q8_page(row, block, c), h, block, c);
-    const uint4* k = reinterpret_cast<const uint4*>(c.k_codes + slot * kQ8Block) + col * 8 + g;
-    const uint4* v = reinterpret_cast<const uint4*>(c.v_codes + slot * kQ8Block) + lane;
+  // A block's registers: key rows 16 tb + col (channels 16 g .. + 15 and 64 + 16 g .. + 15), value slots 64 j + lane,
+  // and the scales, which are wave-uniform. Every address is inside the pool, so the first block is loaded before
+  // the lengths say whether it is needed
+  uint4 k[2][2], v[4];
+  float ks, vs;
+  const uint32_t ko = col * 128 + g * 16, vo = lane * 16;
+  auto load_keys = [&](int64_t slot) {
+    const uint8_t* at = c.k_codes + slot * kQ8Block;
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      x.k[tb][0] = k[tb * 128];
-      x.k[tb][1] = k[tb * 128 + 4];
+      k[tb][0] = *reinterpret_cast<const uint4*>(at + (ko + tb * 2048));
+      k[tb][1] = *reinterpret_cast<const uint4*>(at + (ko + tb * 2048 + 64));
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x.v[j] = v[64 * j];
-    x.ks = c.k_scale[slot];
-    x.vs = c.v_scale[slot];
+    ks = uniform_load(c.k_scale + slot);
   };
+  auto load_values = [&](int64_t slot) {
+    const uint8_t* at = c.v_codes + slot * kQ8Block;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint4*>(at + (vo + j * 1024));
+    vs = uniform_load(c.v_scale + slot);
+  };
+  int64_t slot = q8_slot(q8_page(row, block, c), h, block, c);
+  load_keys(slot);
+  load_values(slot);
+  int page = q8_page(row, block + stride, c);  // of the wave's next block
+
+  const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
+  if (n == 0) return;
+  const int i_last = min((kQ8Cols - 1) / p.G, n - 1);
+  const int vis_first = p.cross ? len : max(len - n + 1, 0);  // tokens that the first and the last row see
+  const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
+  const int i = col / p.G, hq = h * p.G + (col - i * p.G);
+  const bool live = i < n;
+  const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
+  const int nblk = (vis_last + kW - 1) / kW;
 
   // query operands: column's channels 64 (kk / 2) + 16 g + 8 (kk % 2) .. + 7
   half8 qop[4];
   float qs = p.qscale;
   {
-    const uint4* q = reinterpret_cast<const uint4*>(p.q) + (((int64_t)b * c.Hq + hq) * p.n_max + i) * 16;
+    const uint4* q = reinterpret_cast<const uint4*>(p.q) + (live ? ((int64_t)b * c.Hq + hq) * p.n_max + i : 0) * 16;
     uint4 raw[4];
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) raw[kk] = live ? q[8 * (kk >> 1) + 2 * g + (kk & 1)] : make_uint4(0u, 0u, 0u, 0u);
+    for (int kk = 0; kk < 4; ++kk) {
+      raw[kk] = q[8 * (kk >> 1) + 2 * g + (kk & 1)];
+      if (!live) raw[kk] = make_uint4(0u, 0u, 0u, 0u);
+    }
     qs *= query_operands<kBf16>(raw, qop, [](float v) { return max32(max16(v)); });
   }
 
@@ -88,20 +100,25 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
 #pragma unroll
   for (int t = 0; t < 8; ++t) acc[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto compute = [&](int block, const BlockRegs& x) {
-    const int t0 = block * kW;
+  while (block < nblk) {
+    const int t0 = block * kW, next = block + stride;
+    slot = q8_slot(page, h, next, c);
     floatx4 s[2];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
       s[tb] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
-        const uint4 w = x.k[tb][kk >> 1];
+        const uint4 w = k[tb][kk >> 1];
         s[tb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kk & 1 ? widen8<kFmt>(w.z, w.w) : widen8<kFmt>(w.x, w.y), qop[kk], s[tb], 0,
                                                        0, 0);
       }
     }
-    const float sc = x.ks * qs;
+    const float sc = ks * qs;
+    // the keys' registers are free: the next block's keys are on their way during the softmax and the value product,
+    // its values during the next scores. Four waves on a SIMD do the rest; a second set of registers instead left
+    // room for two
+    if (next < nblk) load_keys(slot);
     float mx = -__builtin_inff();
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
@@ -119,10 +136,10 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[tb][e]);
     mx = max32(max16(mx));
-    float lv = __builtin_amdgcn_logf(x.vs);
+    float lv = __builtin_amdgcn_logf(vs);
     // a block whose values are all zero has scale 1: it adds to the sum alone and must not move M (a subnormal
     // scale has lv = -inf here, and the same)
-    if (x.vs == 1.0f && !__any(((or4(x.v[0]) | or4(x.v[1]) | or4(x.v[2]) | or4(x.v[3])) & 0x7f7f7f7fu) != 0)) lv = -__builtin_inff();
+    if (vs == 1.0f && !__any(((or4(v[0]) | or4(v[1]) | or4(v[2]) | or4(v[3])) & 0x7f7f7f7fu) != 0)) lv = -__builtin_inff();
     if (__any(mx > m + kLazy || mx + lv > M + kLazy)) {
       const float m2 = fmaxf(m, mx), M2 = fmaxf(M, mx + lv);
       l *= __builtin_amdgcn_exp2f(m - m2);
@@ -145,23 +162,12 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
     const half8 wop = __builtin_bit_cast(half8, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(x.v[j].x, x.v[j].y), wop, acc[2 * j], 0, 0, 0);
-      acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(x.v[j].z, x.v[j].w), wop, acc[2 * j + 1], 0, 0, 0);
+      acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(v[j].x, v[j].y), wop, acc[2 * j], 0, 0, 0);
+      acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(v[j].z, v[j].w), wop, acc[2 * j + 1], 0, 0, 0);
     }
-  };
-
-  // two register sets: the next block's loads are in flight while one is computed
-  BlockRegs xa, xb;
-  int block = split * kWaves + wave;
-  if (block < nblk) load(block, xa);
-  while (block < nblk) {
-    if (block + stride < nblk) load(block + stride, xb);
-    compute(block, xa);
-    block += stride;
-    if (block >= nblk) break;
-    if (block + stride < nblk) load(block + stride, xa);
-    compute(block, xb);
-    block += stride;
+    if (next < nblk) load_values(slot);
+    page = q8_page(row, next + stride, c);
+    block = next;
   }
 
   // ---- combine the waves ----
@@ -175,7 +181,8 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
   }
   __syncthreads();
   const int cc = tid >> 5, ch = (tid & 31) * 4;
-  const int ci = (r0 + cc) / p.G, chq = h * p.G + (r0 + cc - ci * p.G);
+  static_assert(kThreads == 32 * kQ8Cols, "32 lanes a column");
+  const int ci = cc / p.G, chq = h * p.G + (cc - ci * p.G);
   if (ci >= n) return;
   float Mt = kNoScore, mt = kNoScore;
 #pragma unroll
@@ -190,128 +197,152 @@ __global__ __launch_bounds__(kThreads) void k_q8_split(Q8AttendArgs p) {
     lt += wl[w][cc] * __builtin_amdgcn_exp2f(wm[w][cc] - mt);
     o += *reinterpret_cast<const floatx4*>(&cmb[w][cc * kCombineRow + ch]) * __builtin_amdgcn_exp2f(wM[w][cc] - Mt);
   }
-  if (p.nsplit == 1) {
+  if (records == 0) {
     const float f = lt > 0.0f ? __builtin_amdgcn_exp2f(Mt - mt - kWeightExp) / lt : 0.0f;
     *reinterpret_cast<uint2*>(p.out + (((int64_t)b * c.Hq + chq) * p.n_max + ci) * kD + ch) =
         make_uint2(row_pack<kBf16>(o[0] * f, o[1] * f), row_pack<kBf16>(o[2] * f, o[3] * f));
     return;
   }
-  float* rec = p.ws + (((int64_t)b * gridDim.y + blockIdx.y) * p.nsplit + split) * kRecFloatsQ8;
+  float* rec = p.ws + ((int64_t)first * c.H + h * nsplit + split) * kRecFloatsQ8;
   *reinterpret_cast<floatx4*>(rec + cc * kD + ch) = o;
   if ((tid & 31) == 0) *reinterpret_cast<floatx4*>(rec + kQ8Cols * kD + 4 * cc) = floatx4{Mt, mt, lt, 0.0f};
 }
 
-// Join the splits of one column: 8 groups of 32 lanes take every eighth split, then the groups are added.
-template <bool kBf16>
-__global__ __launch_bounds__(256) void k_q8_merge(Q8AttendArgs p, int cols) {
-  __shared__ float factor[kQ8MaxSplits];
-  __shared__ __attribute__((aligned(16))) floatx4 part[8][32];
-  __shared__ float scale;
-  const int cc = blockIdx.x, h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int n = min(max(p.n_new[b], 0), p.n_max);
+// Join the splits: kGroups groups of 32 lanes share a column's (a group takes every kGroups-th split, then the
+// groups are added), kCols columns a work-group
+template <bool kBf16, int kGroups, int kCols>
+__global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs p, int cols) {
+  __shared__ __attribute__((aligned(16))) floatx4 part[kGroups * kCols][32];
+  const int h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, grp = (tid >> 5) % kGroups, cc = blockIdx.x * kCols + (tid >> 5) / kGroups;
+  const int first = p.splits.first[b], nsplit = p.splits.first[b + 1] - first;
+  if (nsplit == 0) return;
+  const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int r = tile * cols + cc, i = r / p.G, hq = h * p.G + (r - i * p.G);
-  if (i >= n) return;
+  const bool live = i < n;
+  if (kCols == 1 && !live) return;  // the whole work-group
   const int recf = cols * (kD + 4);
-  const float* rec = p.ws + ((int64_t)b * gridDim.y + blockIdx.y) * p.nsplit * recf;
-  if (tid < 64) {
+  const float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit) * recf;
+  floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  float scale = 0.0f;
+  if (live) {
+    // every group forms the references and the sum of all splits (a lane takes every 32nd), and its own factors
+    const float* stat = rec + cols * kD + 4 * cc;
     float M = kNoScore, m = kNoScore, l = 0.0f;
-    float fM[kQ8MaxSplits / 64];
-#pragma unroll
-    for (int k = 0; k < kQ8MaxSplits / 64; ++k) {
-      const int s = lane + 64 * k;
-      floatx4 st = {kNoScore, kNoScore, 0.0f, 0.0f};
-      if (s < p.nsplit) st = *reinterpret_cast<const floatx4*>(rec + (int64_t)s * recf + cols * kD + 4 * cc);
-      fM[k] = st[0];
+    for (int s = lane; s < nsplit; s += 32) {
+      const floatx4 st = *reinterpret_cast<const floatx4*>(stat + (int64_t)s * recf);
       const float m2 = fmaxf(m, st[1]);
       l = l * __builtin_amdgcn_exp2f(m - m2) + st[2] * __builtin_amdgcn_exp2f(st[1] - m2);
       m = m2;
       M = fmaxf(M, st[0]);
     }
-    M = wave_max(M);
-    const float mt = wave_max(m);
-    l *= __builtin_amdgcn_exp2f(m - mt);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-#pragma unroll
-    for (int k = 0; k < kQ8MaxSplits / 64; ++k) factor[lane + 64 * k] = __builtin_amdgcn_exp2f(fM[k] - M);
-    if (lane == 0) scale = l > 0.0f ? __builtin_amdgcn_exp2f(M - mt - kWeightExp) / l : 0.0f;
+    for (int d = 1; d < 32; d <<= 1) {
+      const float m1 = __shfl_xor(m, d), l1 = __shfl_xor(l, d), m2 = fmaxf(m, m1);
+      l = l * __builtin_amdgcn_exp2f(m - m2) + l1 * __builtin_amdgcn_exp2f(m1 - m2);
+      m = m2;
+      M = fmaxf(M, __shfl_xor(M, d));
+    }
+    scale = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
+    const float* sums = rec + cc * kD + 4 * lane;
+#pragma unroll 4
+    for (int s = grp; s < nsplit; s += kGroups)
+      o += *reinterpret_cast<const floatx4*>(sums + (int64_t)s * recf) * __builtin_amdgcn_exp2f(stat[(int64_t)s * recf] - M);
   }
-  __syncthreads();
-  const int grp = tid >> 5, ch = (tid & 31) * 4;
-  floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = grp; s < p.nsplit; s += 8) o += *reinterpret_cast<const floatx4*>(rec + (int64_t)s * recf + cc * kD + ch) * factor[s];
-  part[grp][tid & 31] = o;
-  __syncthreads();
-  if (tid >= 32) return;
+  if constexpr (kGroups > 1) {
+    part[tid >> 5][lane] = o;
+    __syncthreads();
+    if (grp != 0) return;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) o += part[k][tid];
+    for (int k = 1; k < kGroups; ++k) o += part[(tid >> 5) + k][lane];
+  }
+  if (!live) return;
   o *= scale;
-  *reinterpret_cast<uint2*>(p.out + (((int64_t)b * p.c.Hq + hq) * p.n_max + i) * kD + ch) =
+  *reinterpret_cast<uint2*>(p.out + (((int64_t)b * p.c.Hq + hq) * p.n_max + i) * kD + 4 * lane) =
       make_uint2(row_pack<kBf16>(o[0], o[1]), row_pack<kBf16>(o[2], o[3]));
 }
 
 }  // namespace
 
-Q8Plan q8_plan(int B, int H, int G, int n_max, int max_len) {
-  Q8Plan p;
+// Every split takes the same number of tokens at most, the least that needs no more work-groups than fit the GPU at
+// once: a ragged batch is shared evenly (16 sequences of 8704 to 16384 tokens: 46 -> 41 us against as many splits for each).
+// * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
+//   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
+// * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
+//   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
+void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
   const int64_t rows = (int64_t)n_max * G;
-  p.cols = rows <= kQ8Cols ? kQ8Cols : kQ8PromptCols;
+  const bool few = rows <= kQ8Cols;
+  p.cols = few ? kQ8Cols : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
-  const int64_t units = (int64_t)B * H * p.ntile;
-  int64_t want, most;
-  if (p.cols == kQ8Cols) {
-    // work-groups for every compute unit; a split has at least a block for each wave
-    want = (kQ8Groups + units - 1) / units;
-    most = ((max_len + kW - 1) / kW + kWaves - 1) / kWaves;
-  } else {
-    want = (kQ8PromptGroups + units - 1) / units;
-    most = (max_len + kQ8PromptSplit - 1) / kQ8PromptSplit;
+  p.rows = (int)std::min<int64_t>(rows, p.cols);
+  const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
+  const int64_t round = few ? kW * kWaves : kQ8PromptSplit;  // tokens of a round
+  const int64_t units = (int64_t)H * p.ntile;
+  const auto fits = [&](int64_t rounds) {
+    int64_t n = 0;
+    for (int b = 0; b < B; ++b) n += std::max<int64_t>(1, (lens[b] + rounds * round - 1) / (rounds * round));
+    return n * units <= groups;
+  };
+  int longest = 0;
+  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
+  int64_t lo = 1, hi = std::max<int64_t>((longest + round - 1) / round, 1);  // hi rounds: one split each
+  while (lo < hi) {  // the fewest rounds that fit
+    const int64_t mid = (lo + hi) / 2;
+    if (fits(mid)) hi = mid;
+    else lo = mid + 1;
   }
-  p.nsplit = (int)std::max<int64_t>(1, std::min({want, most, (int64_t)kQ8MaxSplits}));
-  return p;
-}
-
-size_t q8_plan_bytes(const Q8Plan& p, int B, int H) {
-  if (p.nsplit == 1) return 0;
-  return (size_t)B * H * p.ntile * p.nsplit * p.cols * (kD + 4) * sizeof(float);
-}
-
-// A call of u units (tiles of every sequence and head) has at most the groups it is split into and u records more;
-// calls of fewer rows have no more units of the same kind, and a call of few rows has B H
-size_t q8_workspace_bound(int B, int H, int G, int n_max, int max_len) {
-  const size_t few = ((size_t)B * H + kQ8Groups) * kQ8Cols;
-  const int64_t rows = (int64_t)n_max * G;
-  size_t many = 0;
-  if (rows > kQ8Cols) {
-    const size_t units = (size_t)B * H * ((rows + kQ8PromptCols - 1) / kQ8PromptCols);
-    many = std::min(units, (size_t)kQ8PromptGroups) + kQ8PromptGroups;  // units of kQ8PromptGroups and more are not split
-    many *= kQ8PromptCols;
+  if (few && longest <= 4 * round) hi = 4;
+  const bool idle = B * units * 64 < 256 && longest > 64 * 4 * round;
+  const int64_t most = idle ? kQ8MaxSplits : 64;
+  p.most = 1;
+  p.splits.first[0] = 0;
+  for (int b = 0; b < B; ++b) {
+    const int s = (int)std::max<int64_t>(1, std::min((lens[b] + hi * round - 1) / (hi * round), most));
+    p.most = std::max(p.most, s);
+    p.splits.first[b + 1] = (uint16_t)(p.splits.first[b] + (s > 1 ? s : 0));
   }
-  (void)max_len;
-  return std::max(few, many) * (kD + 4) * sizeof(float);
 }
 
-hipError_t launch_q8_attention(Q8AttendArgs a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
-  a.nsplit = p.nsplit;
+// A call's splits fit into its groups, but for units (tiles of a sequence and head) that are more than the groups: those
+// have one split and no record. Calls of few rows and of many count by themselves
+size_t q8_workspace_bound(int G, int n_max) {
+  const size_t few = (size_t)kQ8Groups * kQ8Cols, many = (size_t)kQ8PromptGroups * kQ8PromptCols;
+  return ((int64_t)n_max * G > kQ8Cols ? std::max(few, many) : few) * (kD + 4) * sizeof(float);
+}
+
+template <int kGroups, int kCols>
+static void merge(const Q8AttendArgs& a, const Q8Plan& p, int B, bool bf16, hipStream_t s) {
+  // no work-group for columns that no row has
+  const dim3 grid((p.rows + kCols - 1) / kCols, a.c.H * p.ntile, B), block(32 * kGroups * kCols);
+  if (bf16) hipLaunchKernelGGL((k_q8_merge<true, kGroups, kCols>), grid, block, 0, s, a, p.cols);
+  else hipLaunchKernelGGL((k_q8_merge<false, kGroups, kCols>), grid, block, 0, s, a, p.cols);
+}
+
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
   a.ntile = p.ntile;
-  const dim3 grid(p.nsplit, a.c.H * p.ntile, B), block(kThreads);
+  a.splits = p.splits;
   const bool bf16 = dtype == OKVQ_BF16;
   hipError_t e;
   if (p.cols == kQ8PromptCols) {
-    e = launch_q8_prompt(a, format, dtype, B, s);
-  } else if (format == OKVQ_Q8_INT8) {
-    if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
+    e = launch_q8_prompt(a, p.most, format, dtype, B, s);
   } else {
-    if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, false>), grid, block, 0, s, a);
+    const dim3 grid(p.most, a.c.H, B), block(kThreads);
+    if (format == OKVQ_Q8_INT8) {
+      if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
+    } else {
+      if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, true>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, false>), grid, block, 0, s, a);
+    }
+    e = hipGetLastError();
   }
-  if (p.cols == kQ8Cols) e = hipGetLastError();
-  if (e != hipSuccess || p.nsplit == 1) return e;
-  const dim3 mgrid(p.cols, a.c.H * p.ntile, B);
-  if (bf16) hipLaunchKernelGGL((k_q8_merge<true>), mgrid, dim3(256), 0, s, a, p.cols);
-  else hipLaunchKernelGGL((k_q8_merge<false>), mgrid, dim3(256), 0, s, a, p.cols);
+  if (e != hipSuccess || p.most == 1) return e;
+  // a column to 8 groups of lanes, 16 where there are many splits (128 splits: 7.9 -> 4.5 us); 8 columns to a work-group
+  // where there are few (2 splits of 32768 rows: 33 -> 8 us)
+  if (p.most > 64) merge<16, 1>(a, p, B, bf16, s);
+  else if (p.most > 8 || p.cols == kQ8Cols) merge<8, 1>(a, p, B, bf16, s);
+  else merge<1, 8>(a, p, B, bf16, s);
   return hipGetLastError();
 }
 

@@ -45,10 +45,12 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   // which see most, start first
   const int units = B * c.H, unit = blockIdx.x % units, split = blockIdx.y;
   const int tile = p.ntile - 1 - (int)(blockIdx.x / units), b = unit / c.H, h = unit - b * c.H;
+  const int first = p.splits.first[b], records = p.splits.first[b + 1] - first, nsplit = max(records, 1);
+  if (split >= nsplit) return;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + (int64_t)b * c.max_pages;
-  const int len = q8_len(c, b), n = min(max(p.n_new[b], 0), p.n_max);
+  const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int r0 = tile * kQ8PromptCols, i_first = r0 / p.G;
   if (i_first >= n) return;
   const int i_last = min((r0 + kQ8PromptCols - 1) / p.G, n - 1);
@@ -60,17 +62,19 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   const int wave_first = (r0 + 32 * wave) / p.G;
   const int vis_first = wave_first >= n ? 0 : p.cross ? len : max(len - n + wave_first + 1, 0);
   const int ntile = (vis_last + kTile - 1) / kTile;
-  const int per = (ntile + p.nsplit - 1) / p.nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
+  const int per = (ntile + nsplit - 1) / nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
 
   // staging: thread tid has 16 bytes of key row tid / 8 and value slot tid % 256 of block tid / 256
   const int sb = wave >> 2, krow = (tid >> 3) & 31, kchunk = tid & 7, vslot = tid & 255;
+  int page = q8_page(table, 2 * t_begin + sb, c);
   auto load = [&](int t, Raw& x) {
     const int block = 2 * t + sb;  // may lie behind the sequence: then codes of any page inside the pool, all masked
-    const int64_t slot = q8_slot(q8_page(table, block, c), h, block, c);
-    x.k = reinterpret_cast<const uint4*>(c.k_codes + slot * kQ8Block)[tid & 255];
-    x.v = reinterpret_cast<const uint4*>(c.v_codes + slot * kQ8Block)[vslot];
-    x.ks = c.k_scale[slot];
-    x.vs = c.v_scale[slot];
+    const int64_t slot = q8_slot(page, h, block, c);
+    x.k = *reinterpret_cast<const uint4*>(c.k_codes + slot * kQ8Block + vslot * 16);
+    x.v = *reinterpret_cast<const uint4*>(c.v_codes + slot * kQ8Block + vslot * 16);
+    x.ks = uniform_load(c.k_scale + slot);
+    x.vs = uniform_load(c.v_scale + slot);
+    page = q8_page(table, block + 2, c);  // of the next call's block
     if (block * kW >= len) {  // what is multiplied by a zero weight has to be finite
       x.k = x.v = make_uint4(0u, 0u, 0u, 0u);
       x.ks = x.vs = 1.0f;
@@ -200,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
 
   l = sum32(l);
   if (!live) return;
-  if (p.nsplit == 1) {
+  if (records == 0) {
     const float f = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
     uint16_t* out = p.out + (((int64_t)b * c.Hq + hq) * p.n_max + i) * kD + 4 * half;
 #pragma unroll
@@ -211,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
                                                                      row_pack<kBf16>(acc[j][e + 2] * f, acc[j][e + 3] * f));
     return;
   }
-  float* rec = p.ws + (((int64_t)unit * p.ntile + tile) * p.nsplit + split) * (kQ8PromptCols * (kD + 4));
+  float* rec = p.ws + ((int64_t)first * c.H * p.ntile + ((int64_t)h * p.ntile + tile) * nsplit + split) * (kQ8PromptCols * (kD + 4));
   const int cc = 32 * wave + col;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -224,8 +228,8 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
 
 }  // namespace
 
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, int format, int dtype, int B, hipStream_t s) {
-  const dim3 grid((unsigned)(B * a.c.H * a.ntile), a.nsplit), block(kThreads);
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, int most, int format, int dtype, int B, hipStream_t s) {
+  const dim3 grid((unsigned)(B * a.c.H * a.ntile), most), block(kThreads);
   if (format == OKVQ_Q8_INT8) {
     if (dtype == OKVQ_BF16) hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_INT8, true>), grid, block, 0, s, a, B);
     else hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_INT8, false>), grid, block, 0, s, a, B);

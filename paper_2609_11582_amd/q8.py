@@ -5,6 +5,7 @@ type; the stream is torch's current one unless one is given."""
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Sequence
 
 import torch
@@ -21,6 +22,7 @@ OKVQ_Q8_E4M3 = 1
 OKVQ_Q8_CROSS = 1         # every row sees the whole sequence
 Q8_FORMATS = {"int8": OKVQ_Q8_INT8, "e4m3": OKVQ_Q8_E4M3}
 Q8_DTYPES = {"fp16": (OKVQ_F16, torch.float16), "bf16": (OKVQ_BF16, torch.bfloat16)}
+_ROW_TYPES = {torch.float16: OKVQ_F16, torch.bfloat16: OKVQ_BF16}
 # buffer ids 0..9 of okvq_q8_buffer_bytes (OKVQ_Q8_BUF_*)
 Q8_BUFFERS = ("k_codes", "v_codes", "k_scale", "v_scale", "k_stage", "v_stage", "block_table", "seq_lens", "page_refs",
               "status")
@@ -53,8 +55,8 @@ def lib() -> ctypes.CDLL:
         L = _okvq_lib()
         vp, i32, u32, sz, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t, ctypes.POINTER
         for name, res, args in (
-                ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, P(Rows), P(Rows), vp, P(i32), P(Rows), P(Rows), i32,
-                                      u32, vp]),
+                # okvq_rows as packed bytes (_rows_of) or Rows structures
+                ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, P(i32), vp, vp, i32, u32, vp]),
                 ("okvq_q8_buffer_bytes", sz, [P(Q8Dims), i32]),
                 ("okvq_q8_append", i32, [P(Q8Struct), i32, P(i32), vp, vp, P(i32), vp, i32, vp]),
                 ("okvq_q8_workspace_bytes", sz, [P(Q8Dims), i32, i32]),
@@ -71,22 +73,35 @@ def lib() -> ctypes.CDLL:
     return _ready
 
 
-def _need(t: torch.Tensor, nbytes: int, dtype, name: str) -> int:
+# Host time of a call counts at a decode step: the checks below read each property of a tensor once, and a call asks
+# for the current device once.
+_device = torch.cuda.current_device
+
+
+def _need(t: torch.Tensor, nbytes: int, dtype, name: str, device: int) -> int:
     """The tensor's address, once it is contiguous, on the current device, of the type and large enough."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous device tensor")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is {torch.cuda.current_device()}")
+    if not isinstance(t, torch.Tensor) or not t.is_contiguous() or t.get_device() != device:
+        _refuse(t, name, device)
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
-    have = t.numel() * t.element_size()
-    if have < nbytes:
-        raise ValueError(f"{name}: {have} bytes, at least {nbytes} needed")
+    if t.nbytes < nbytes:
+        raise ValueError(f"{name}: {t.nbytes} bytes, at least {nbytes} needed")
     return t.data_ptr()
 
 
-def _workspace(t: torch.Tensor, name: str):
-    return _need(t, 0, None, name), t.numel() * t.element_size()
+def _refuse(t, name: str, device: int):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous device tensor")
+    raise ValueError(f"{name}: on {t.device}, but the current device is {device}")
+
+
+def _ints(xs: Sequence[int], n: int, name: str):
+    if len(xs) != n:
+        raise ValueError(f"{name}: {len(xs)} entries, expected {n}")
+    try:
+        return (ctypes.c_int32 * n)(*xs)
+    except TypeError:  # numpy integers and the like
+        return _i32(xs)
 
 
 # ---- rotary positions ----------------------------------------------------------------------------
@@ -101,18 +116,19 @@ def make_rotary(inv_freq: Sequence[float], axes: Sequence[int]) -> RotaryParams:
     return RotaryParams((ctypes.c_double * 64)(*[float(f) for f in inv_freq]), (ctypes.c_uint8 * 64)(*[int(a) for a in axes]))
 
 
-def _rows_of(t: torch.Tensor, batch: int, tokens: int, dtype, name: str) -> Rows:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 4 or t.shape[3] != 128:
-        raise ValueError(f"{name}: expected a device tensor [batch][heads][tokens][128]")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, but the current device is {torch.cuda.current_device()}")
-    if t.shape[0] != batch or t.shape[2] != tokens or t.dtype != dtype:
-        raise ValueError(f"{name}: {list(t.shape)} {t.dtype}, expected batch {batch}, {tokens} tokens, {dtype}")
-    if t.stride(3) != 1:
+_pack_rows = struct.Struct("Pqqq").pack  # the layout of Rows
+
+
+def _rows_of(t: torch.Tensor, shape, dtype, name: str, device: int) -> bytes:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        raise ValueError(f"{name}: expected a tensor on the current device {device}")
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name}: {list(t.shape)} {t.dtype}, expected {list(shape)} {dtype}")
+    b, h, n, c = t.stride()
+    if c != 1:
         raise ValueError(f"{name}: the channels of a row have to lie side by side")
     # the stride of a dimension of one entry is whatever torch left there: it moves nothing
-    s = [t.stride(d) if t.shape[d] > 1 else 0 for d in range(3)]
-    return Rows(t.data_ptr(), s[0], s[1], s[2])
+    return _pack_rows(t.data_ptr(), b if shape[0] > 1 else 0, h if shape[1] > 1 else 0, n if shape[2] > 1 else 0)
 
 
 def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, flags=0, stream=None, check=True) -> int:
@@ -121,27 +137,29 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
     positions int32 [batch][3][tokens]; lens: rows of each sequence (None: all). In place where an output is its
     input."""
     some = q if q is not None else k
-    if not isinstance(some, torch.Tensor) or some.dim() != 4 or some.dtype not in (torch.float16, torch.bfloat16):
-        raise ValueError("q, k: expected fp16 or bf16 tensors [batch][heads][tokens][128]")
-    B, n, dt = some.shape[0], some.shape[2], some.dtype
-    rows = []
-    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
-        if (x is None) != (y is None):
-            raise ValueError(f"{name}: an input and an output, or neither")
-        if x is not None and y.shape != x.shape:
-            raise ValueError(f"{name}_out: {list(y.shape)}, expected {list(x.shape)}")
-        rows.append((None, None) if x is None else (_rows_of(x, B, n, dt, name), _rows_of(y, B, n, dt, name + "_out")))
-    (rq, oq), (rk, ok) = rows
-    pos = _need(positions, B * 3 * n * 4, torch.int32, "positions")
-    if tuple(positions.shape) != (B, 3, n):
+    if (not isinstance(some, torch.Tensor) or not some.is_cuda or some.dim() != 4 or some.dtype not in _ROW_TYPES
+            or some.shape[3] != 128):
+        raise ValueError("q, k: expected fp16 or bf16 device tensors [batch][heads][tokens][128]")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q, k: an input and an output of each, or neither")
+    B, _, n, _ = some.shape
+    dt, device = some.dtype, _device()
+    rq = oq = rk = ok = None
+    hq = hk = 0
+    if q is not None:
+        shape = q.shape
+        hq = shape[1]
+        rq, oq = _rows_of(q, shape, dt, "q", device), _rows_of(q_out, shape, dt, "q_out", device)
+    if k is not None:
+        hk = k.shape[1] if isinstance(k, torch.Tensor) and k.dim() == 4 else 0
+        shape = (B, hk, n, 128)
+        rk, ok = _rows_of(k, shape, dt, "k", device), _rows_of(k_out, shape, dt, "k_out", device)
+    pos = _need(positions, 0, torch.int32, "positions", device)
+    if positions.shape != (B, 3, n):
         raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
-    if lens is not None:
-        _need_len(lens, B, "lens")
-    ref = lambda r: None if r is None else ctypes.byref(r)  # noqa: E731
-    st = lib().okvq_rotary(ctypes.byref(rotary), B, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], n, ref(rq),
-                           ref(rk), pos, None if lens is None else _i32(lens), ref(oq), ref(ok),
-                           OKVQ_F16 if dt == torch.float16 else OKVQ_BF16, int(flags), _stream(stream))
-    if check:
+    st = lib().okvq_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, pos, None if lens is None else _ints(lens, B, "lens"),
+                           oq, ok, _ROW_TYPES[dt], flags, _stream(stream))
+    if check and st:
         _check(st, "okvq_rotary")
     return st
 
@@ -182,35 +200,35 @@ class Q8Cache:
                 raise OkvqError(-1, f"okvq_q8_buffer_bytes({name})")
             if buffers is not None:
                 t = buffers[name]
-                _need(t, nbytes, dt, name)
+                _need(t, nbytes, dt, name, _device())
             else:
                 t = torch.full(shapes[name], -1 if name == "block_table" else 0, dtype=dt, device=device)
             self.buffers[name] = t
         self.struct = Q8Struct(self.dims, *[self.buffers[n].data_ptr() for n in Q8_BUFFERS])
         self.device_index = self.buffers["k_codes"].get_device()
+        self._ref = ctypes.byref(self.struct)
+        self._sizes = batch, num_kv_heads, num_q_heads
 
     def __getitem__(self, name):
         return self.buffers[name]
 
 
-def _cache_ref(cache: Q8Cache):
-    if cache.device_index != torch.cuda.current_device():
-        raise ValueError(f"cache: on device {cache.device_index}, but the current device is {torch.cuda.current_device()}")
-    return ctypes.byref(cache.struct)
+def _cache_ref(cache: Q8Cache, device: int):
+    if cache.device_index != device:
+        raise ValueError(f"cache: on device {cache.device_index}, but the current device is {device}")
+    return cache._ref
 
 
 def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, n_max, stream=None, check=True) -> int:
     """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128]) into one layer's pages, after
     okvq_q8_extend; lens: the lengths with them."""
-    d = cache.dims
-    ref = _cache_ref(cache)
-    _need_len(lens, d.batch, "lens")
-    _need_len(n_new, d.batch, "n_new")
-    nbytes = d.batch * d.num_kv_heads * int(n_max) * 256
-    st = lib().okvq_q8_append(ref, int(layer), _i32(lens), _need(k_new, nbytes, cache.row_dtype, "k_new"),
-                              _need(v_new, nbytes, cache.row_dtype, "v_new"), _i32(n_new),
-                              _need(n_new_dev, d.batch * 4, torch.int32, "n_new_dev"), int(n_max), _stream(stream))
-    if check:
+    B, H, _ = cache._sizes
+    dev, dt = _device(), cache.row_dtype
+    nbytes = B * H * n_max * 256
+    st = lib().okvq_q8_append(_cache_ref(cache, dev), layer, _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
+                              _need(v_new, nbytes, dt, "v_new", dev), _ints(n_new, B, "n_new"),
+                              _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_append")
     return st
 
@@ -229,16 +247,14 @@ def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, s
                       stream=None, check=True) -> int:
     """Attention of rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
     tokens of each sequence, causal, or OKVQ_Q8_CROSS. lens: the lengths with the new tokens."""
-    d = cache.dims
-    ref = _cache_ref(cache)
-    _need_len(lens, d.batch, "lens")
-    _need_len(n_new, d.batch, "n_new")
-    nbytes = d.batch * d.num_q_heads * int(n_max) * 256
-    ws, ws_bytes = _workspace(workspace, "workspace")
-    st = lib().okvq_q8_attention(ref, int(layer), _i32(lens), _need(q, nbytes, cache.row_dtype, "q"), _i32(n_new),
-                                 _need(n_new_dev, d.batch * 4, torch.int32, "n_new_dev"), int(n_max), float(sm_scale),
-                                 _need(out, nbytes, cache.row_dtype, "out"), ws, ws_bytes, int(flags), _stream(stream))
-    if check:
+    B, _, Hq = cache._sizes
+    dev, dt = _device(), cache.row_dtype
+    nbytes = B * Hq * n_max * 256
+    st = lib().okvq_q8_attention(_cache_ref(cache, dev), layer, _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
+                                 _ints(n_new, B, "n_new"), _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, sm_scale,
+                                 _need(out, nbytes, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
+                                 flags, _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_attention")
     return st
 
@@ -255,39 +271,39 @@ def q8_page_workspace(dims: Q8Dims, device="cuda") -> torch.Tensor:
 def okvq_q8_extend(cache: Q8Cache, n_new_dev, granted, workspace, stream=None, check=True) -> int:
     """Pages for n_new_dev[b] more tokens in every slot and the lengths advanced by them; granted (int32 [B], device):
     the same counts, or 0 for all where pages are short."""
-    B = cache.dims.batch
-    ref = _cache_ref(cache)
-    ws, ws_bytes = _workspace(workspace, "workspace")
-    st = lib().okvq_q8_extend(ref, _need(n_new_dev, B * 4, torch.int32, "n_new_dev"),
-                              _need(granted, B * 4, torch.int32, "granted"), ws, ws_bytes, _stream(stream))
-    if check:
+    dev, nbytes = _device(), cache._sizes[0] * 4
+    st = lib().okvq_q8_extend(_cache_ref(cache, dev), _need(n_new_dev, nbytes, torch.int32, "n_new_dev", dev),
+                              _need(granted, nbytes, torch.int32, "granted", dev), _need(workspace, 0, None, "workspace", dev),
+                              workspace.nbytes, _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_extend")
     return st
 
 
 def okvq_q8_fork(cache: Q8Cache, src, dst, stream=None, check=True) -> int:
     """Slot dst[i] becomes a copy of slot src[i] that shares its pages."""
-    _need_len(dst, len(src), "dst")
-    st = lib().okvq_q8_fork(_cache_ref(cache), _i32(src), _i32(dst), len(src), _stream(stream))
-    if check:
+    n = len(src)
+    st = lib().okvq_q8_fork(_cache_ref(cache, _device()), _ints(src, n, "src"), _ints(dst, n, "dst"), n, _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_fork")
     return st
 
 
 def okvq_q8_free(cache: Q8Cache, slots, stream=None, check=True) -> int:
     """Empty slots; pages without another holder are free."""
-    st = lib().okvq_q8_free(_cache_ref(cache), _i32(slots), len(slots), _stream(stream))
-    if check:
+    n = len(slots)
+    st = lib().okvq_q8_free(_cache_ref(cache, _device()), _ints(slots, n, "slots"), n, _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_free")
     return st
 
 
 def okvq_q8_compact(cache: Q8Cache, workspace, stream=None, check=True) -> int:
     """Move the pages in use to the front of the pool."""
-    ref = _cache_ref(cache)
-    ws, ws_bytes = _workspace(workspace, "workspace")
-    st = lib().okvq_q8_compact(ref, ws, ws_bytes, _stream(stream))
-    if check:
+    dev = _device()
+    st = lib().okvq_q8_compact(_cache_ref(cache, dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
+                               _stream(stream))
+    if check and st:
         _check(st, "okvq_q8_compact")
     return st
 
@@ -295,5 +311,5 @@ def okvq_q8_compact(cache: Q8Cache, workspace, stream=None, check=True) -> int:
 def okvq_q8_status(cache: Q8Cache, stream=None):
     """(1 once an extend was short of pages, pages in use after the last compaction). Synchronizes `stream`."""
     words = (ctypes.c_int32 * 2)()
-    _check(lib().okvq_q8_status(_cache_ref(cache), words, _stream(stream)), "okvq_q8_status")
+    _check(lib().okvq_q8_status(_cache_ref(cache, _device()), words, _stream(stream)), "okvq_q8_status")
     return int(words[0]), int(words[1])
