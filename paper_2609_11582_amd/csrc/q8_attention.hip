@@ -270,6 +270,8 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 //   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
 //   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
+// * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
+//   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
 void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
   const int64_t rows = (int64_t)n_max * G;
   const bool few = rows <= kQ8Cols;
@@ -277,15 +279,15 @@ void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
   p.rows = (int)std::min<int64_t>(rows, p.cols);
   const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
-  const int64_t round = few ? kW * kWaves : kQ8PromptSplit;  // tokens of a round
+  int longest = 0;
+  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
+  const int64_t round = few ? kW * kWaves : longest < 4096 ? 512 : 256;  // tokens of a round
   const int64_t units = (int64_t)H * p.ntile;
   const auto fits = [&](int64_t rounds) {
     int64_t n = 0;
     for (int b = 0; b < B; ++b) n += std::max<int64_t>(1, (lens[b] + rounds * round - 1) / (rounds * round));
     return n * units <= groups;
   };
-  int longest = 0;
-  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
   int64_t lo = 1, hi = std::max<int64_t>((longest + round - 1) / round, 1);  // hi rounds: one split each
   while (lo < hi) {  // the fewest rounds that fit
     const int64_t mid = (lo + hi) / 2;

@@ -17,7 +17,6 @@ constexpr float kWeightExp = 7.0f;   // weights are at most 2^(kLazy + kWeightEx
 constexpr int kQ8MaxSplits = 128;
 constexpr int kQ8Groups = 512;       // work-groups that a call of few rows is split into
 constexpr int kQ8PromptGroups = 256; // and a call of many: one for each compute unit
-constexpr int kQ8PromptSplit = 512;  // least tokens of a split of the prompt kernel
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const half2v v = {(_Float16)lo, (_Float16)hi};

@@ -27,19 +27,18 @@ constexpr int kTile = 64;                 // tokens
 constexpr int kOperand = 64;              // 16-byte slots of a matrix operand
 static_assert(kQ8PromptCols == 32 * kWaves, "32 columns a wave");
 
-struct Tile {                             // one buffer
-  uint4 k[2][8][kOperand];                // [block][16 channels][half h, token]: token's place is token ^ (channels & 7)
-  uint4 v[2][4][2][kOperand];             // [block][32 channels][step s][half h, channel]
-  float ks[2], vs[2];
-};
-struct Raw {                              // a thread's 16 bytes of keys and of values
-  uint4 k, v;
-  float ks, vs;
+struct Raw {                              // a thread's 16 bytes of keys or of values, and the block's scale
+  uint4 x;
+  float scale;
+  uint32_t keep;
 };
 
 template <int kFmt, bool kBf16>
 __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
-  __shared__ Tile buf[2];
+  // two buffers of keys [block][16 channels][half h, token: at token ^ (channels & 7)] and of values
+  // [block][32 channels][step s][half h, channel], as operands; the scales of three tiles, as the keys are ahead
+  __shared__ uint4 kbuf[2][2][8][kOperand], vbuf[2][2][4][2][kOperand];
+  __shared__ float kscale[3][2], vscale[2][2];
   const Q8View& c = p.c;
   // sequences and heads vary fastest: work-groups go round the 8 XCDs, so a head's tiles meet in few L2s; the last rows,
   // which see most, start first
@@ -61,36 +60,35 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
   const int wave_first = (r0 + 32 * wave) / p.G;
   const int vis_first = wave_first >= n ? 0 : p.cross ? len : max(len - n + wave_first + 1, 0);
+  const bool busy = wave_first < n;  // a wave without a live column has only its part of the tiles to bring
   const int ntile = (vis_last + kTile - 1) / kTile;
   const int per = (ntile + nsplit - 1) / nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
 
   // staging: thread tid has 16 bytes of key row tid / 8 and value slot tid % 256 of block tid / 256
   const int sb = wave >> 2, krow = (tid >> 3) & 31, kchunk = tid & 7, vslot = tid & 255;
-  int page = q8_page(table, 2 * t_begin + sb, c);
-  auto load = [&](int t, Raw& x) {
-    const int block = 2 * t + sb;  // may lie behind the sequence: then codes of any page inside the pool, all masked
-    const int64_t slot = q8_slot(page, h, block, c);
-    x.k = *reinterpret_cast<const uint4*>(c.k_codes + slot * kQ8Block + vslot * 16);
-    x.v = *reinterpret_cast<const uint4*>(c.v_codes + slot * kQ8Block + vslot * 16);
-    x.ks = uniform_load(c.k_scale + slot);
-    x.vs = uniform_load(c.v_scale + slot);
-    page = q8_page(table, block + 2, c);  // of the next call's block
-    if (block * kW >= len) {  // what is multiplied by a zero weight has to be finite
-      x.k = x.v = make_uint4(0u, 0u, 0u, 0u);
-      x.ks = x.vs = 1.0f;
-    }
+  // A block that lies behind the sequence is read from some page of the pool, and zeroed on its way to LDS: what a zero
+  // weight multiplies has to be finite. Values of a subnormal scale count as zero too: their logarithm is none.
+  auto load = [&](int t, const uint8_t* codes, const float* scales, float least, Raw& r) {
+    const int block = 2 * t + sb;
+    const int64_t slot = q8_slot(q8_page(table, block, c), h, block, c);
+    r.x = *reinterpret_cast<const uint4*>(codes + slot * kQ8Block + vslot * 16);
+    r.scale = uniform_load(scales + slot);
+    r.keep = block * kW < len && r.scale >= least ? ~0u : 0u;
+    r.scale = r.keep ? r.scale : 1.0f;
   };
-  auto store = [&](Tile& t, const Raw& x) {
+  auto load_keys = [&](int t, Raw& r) { load(t, c.k_codes, c.k_scale, 0.0f, r); };
+  auto load_values = [&](int t, Raw& r) { load(t, c.v_codes, c.v_scale, 0x1p-126f, r); };
+  auto store_keys = [&](int u, const Raw& r) {
     const int kp = krow ^ kchunk;
-    t.k[sb][kchunk][kp] = __builtin_bit_cast(uint4, widen8<kFmt>(x.k.x, x.k.y));
-    t.k[sb][kchunk][32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(x.k.z, x.k.w));
+    kbuf[u & 1][sb][kchunk][kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.x & r.keep, r.x.y & r.keep));
+    kbuf[u & 1][sb][kchunk][32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.z & r.keep, r.x.w & r.keep));
+    kscale[u % 3][sb] = r.scale;  // every lane writes the same
+  };
+  auto store_values = [&](int u, const Raw& r) {
     const int j = vslot >> 6, g = (vslot >> 4) & 3, ch = vslot & 15;
-    t.v[sb][j][g >> 1][32 * (g & 1) + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(x.v.x, x.v.y));
-    t.v[sb][j][g >> 1][32 * (g & 1) + 16 + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(x.v.z, x.v.w));
-    if (krow == 0 && kchunk == 0) {
-      t.ks[sb] = x.ks;
-      t.vs[sb] = x.vs;
-    }
+    vbuf[u & 1][sb][j][g >> 1][32 * (g & 1) + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.x & r.keep, r.x.y & r.keep));
+    vbuf[u & 1][sb][j][g >> 1][32 * (g & 1) + 16 + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.z & r.keep, r.x.w & r.keep));
+    vscale[u & 1][sb] = r.scale;
   };
 
   // query operands: column's channels 16 kk + 8 half .. + 7
@@ -118,87 +116,138 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[j][e] = 0.0f;
 
-  Raw raw;
-  if (t_begin < t_end) {
-    load(t_begin, raw);
-    store(buf[0], raw);
-    if (t_begin + 1 < t_end) load(t_begin + 1, raw);
-  }
-  __syncthreads();
-  for (int t = t_begin; t < t_end; ++t) {
-    const Tile& x = buf[(t - t_begin) & 1];
-    floatx16 s[2];
+  // The loop runs the next tile's scores beside this tile's softmax: matrix and vector instructions of one wave overlap
+  // where they do not depend on each other. So the keys in LDS are a tile ahead of the values.
+  const int nt = t_end - t_begin;
+  Raw kr, vr;
+  floatx16 s[2], s2[2];
+  float top[2] = {kNoScore, kNoScore};  // largest dot of each block of s
+  auto scores = [&](const uint4 (&k)[2][8][kOperand], floatx16 (&d)[2]) {
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[tb][e] = 0.0f;
+      for (int e = 0; e < 16; ++e) d[tb][e] = 0.0f;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
-        s[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, x.k[tb][kk][32 * half + (col ^ kk)]), qop[kk], s[tb],
-                                                       0, 0, 0);
+        d[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, k[tb][kk][32 * half + (col ^ kk)]), qop[kk], d[tb], 0,
+                                                       0, 0);
     }
-    if (t + 1 < t_end) {
-      store(buf[(t + 1 - t_begin) & 1], raw);
-      if (t + 2 < t_end) load(t + 2, raw);
-    }
+  };
+  auto tops = [&](const floatx16 (&d)[2]) {
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      const int t0 = t * kTile + tb * kW;
-      const float sc = fmaxf(x.ks[tb] * qs, 1e-37f), vs = x.vs[tb];  // above zero: a masked dot stays -inf
-      if (t0 + kW > vis_first) {  // a token that some column of the wave does not see
+      float x = d[tb][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) x = fmaxf(x, d[tb][e]);
+      top[tb] = max32(x);
+    }
+  };
+  if (nt > 0) {
+    load_keys(t_begin, kr);
+    load_values(t_begin, vr);
+    store_keys(0, kr);
+    store_values(0, vr);
+    load_keys(t_begin + 1, kr);
+    load_values(t_begin + 1, vr);
+    store_keys(1, kr);
+    load_keys(t_begin + 2, kr);
+    __syncthreads();
+    if (busy) {
+      scores(kbuf[0], s);
+      tops(s);
+    }
+    __syncthreads();  // the first pass of the loop overwrites that buffer
+  }
+  auto stage = [&](int u) {
+    store_values(u + 1, vr);
+    store_keys(u + 2, kr);
+    load_values(t_begin + u + 2, vr);
+    load_keys(t_begin + u + 3, kr);
+  };
+  for (int u = 0; u < nt; ++u) {
+    if (!busy) {
+      stage(u);
+      __syncthreads();
+      continue;
+    }
+    const int cur = u & 1, t0 = (t_begin + u) * kTile;
+    if (t0 + kTile > vis_first) {  // a token that some column of the wave does not see
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (t0 + 8 * (e >> 2) + 4 * half + (e & 3) >= vis) s[tb][e] = -__builtin_inff();
-      }
-      float top = s[tb][0];
+          if (t0 + tb * kW + 8 * (e >> 2) + 4 * half + (e & 3) >= vis) s[tb][e] = -__builtin_inff();
+      tops(s);
+    }
+    float sc[2], lv[2], high[2], reach[2], off[2], gain[2];
+    bool dead[2] = {false, false};
 #pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[tb][e]);
-      top = max32(top) * sc;
-      const float lv = __builtin_amdgcn_logf(vs);
-      // a block whose values are all zero (its scale is 1 then), or have a subnormal scale, adds to the sum alone
-      bool dead = lv < -126.0f;
-      if (vs == 1.0f) {
+    for (int tb = 0; tb < 2; ++tb) {
+      sc[tb] = fmaxf(kscale[u % 3][tb] * qs, 1e-37f);  // above zero: a masked dot stays -inf
+      lv[tb] = __builtin_amdgcn_logf(vscale[cur][tb]);
+    }
+    if (vscale[cur][0] == 1.0f || vscale[cur][1] == 1.0f) {
+      // a block whose values are all zero (its scale is 1 then) adds to the sum alone and must not move M
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
         uint32_t any = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int st = 0; st < 2; ++st) any |= or4(x.v[tb][j][st][lane]);
-        dead = !__any((any & 0x7fff7fffu) != 0);
-      }
-      const float reach = dead ? -__builtin_inff() : top + lv;
-      if (__any(top > m + kLazy || reach > M + kLazy)) {
-        const float m2 = fmaxf(m, top), M2 = fmaxf(M, reach);
-        l *= __builtin_amdgcn_exp2f(m - m2);
-        const float f = __builtin_amdgcn_exp2f(M - M2);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] *= f;
-        m = m2;
-        M = M2;
-      }
-      const float off = dead ? -m : lv + kWeightExp - M;
-      float sum = 0.0f;
-      uint32_t w[8];
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][e], sc, off));
-        const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][e + 1], sc, off));
-        sum += w0 + w1;
-        w[e >> 1] = pack_f16(w0, w1);
-      }
-      l = __builtin_fmaf(sum, __builtin_amdgcn_exp2f(fminf(-off - m, 126.0f)), l);
-      if (dead) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = 0u;
-      }
-      // step s takes tokens 8 s + 4 half + i and 16 + 8 s + 4 half + i: elements 4 s + i and 8 + 4 s + i
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const half8 wop = __builtin_bit_cast(half8, make_uint4(w[2 * st], w[2 * st + 1], w[4 + 2 * st], w[5 + 2 * st]));
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, x.v[tb][j][st][lane]), wop, acc[j], 0, 0, 0);
+          for (int st = 0; st < 2; ++st) any |= or4(vbuf[cur][tb][j][st][lane]);
+        dead[tb] = !__any((any & 0x7fff7fffu) != 0);
       }
     }
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      high[tb] = top[tb] * sc[tb];
+      reach[tb] = dead[tb] ? -__builtin_inff() : high[tb] + lv[tb];
+    }
+    const float high2 = fmaxf(high[0], high[1]), reach2 = fmaxf(reach[0], reach[1]);
+    if (__any(high2 > m + kLazy || reach2 > M + kLazy)) {
+      const float m2 = fmaxf(m, high2), M2 = fmaxf(M, reach2);
+      l *= __builtin_amdgcn_exp2f(m - m2);
+      const float f = __builtin_amdgcn_exp2f(M - M2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] *= f;
+      m = m2;
+      M = M2;
+    }
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      off[tb] = dead[tb] ? -m : lv[tb] + kWeightExp - M;  // zero codes take any finite weight
+      gain[tb] = __builtin_amdgcn_exp2f(fminf(-off[tb] - m, 126.0f));
+    }
+    // One stretch without a branch: the next scores beside this tile's weights, then the value product beside the next
+    // scores' maxima and the tiles to come on their way to LDS (behind the last tile they are some page's, and unused)
+    scores(kbuf[cur ^ 1], s2);
+    uint32_t w[2][8];
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][e], sc[tb], off[tb]));
+        const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tb][e + 1], sc[tb], off[tb]));
+        sum += w0 + w1;
+        w[tb][e >> 1] = pack_f16(w0, w1);
+      }
+      l = __builtin_fmaf(sum, gain[tb], l);
+    }
+    stage(u);
+    // step st takes tokens 8 st + 4 half + i and 16 + 8 st + 4 half + i: elements 4 st + i and 8 + 4 st + i
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const half8 wop = __builtin_bit_cast(half8, make_uint4(w[tb][2 * st], w[tb][2 * st + 1], w[tb][4 + 2 * st], w[tb][5 + 2 * st]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vbuf[cur][tb][j][st][lane]), wop, acc[j], 0, 0, 0);
+      }
+    s[0] = s2[0];
+    s[1] = s2[1];
+    tops(s);
     __syncthreads();
   }
 
