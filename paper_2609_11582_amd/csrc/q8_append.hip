@@ -9,18 +9,40 @@
 // + 3 of channels 4 cgrp .. + 3 of both kinds: 8-byte loads, 32 lanes to a 256-byte row. A key store is then 4
 // bytes a row, a value dword is one channel's 4 tokens; the values pass through LDS to leave in whole 16-byte
 // slots of the operand order.
+#include <type_traits>
+
 #include "q8.hpp"
+#include "wave_ops.hpp"
 
 namespace okvq {
 namespace {
 
 constexpr int kThreads = 256;
 
-// code of t = fl(x / scale), clamped
-template <int kFmt>
-__device__ __forceinline__ float q8_ratio(float x, float scale) {
+// fl(x / scale) for many x of one scale: the quotient by the scale's correctly rounded reciprocal y, corrected twice by
+// its remainder (Markstein's theorem: the first step leaves a faithful quotient, the second the correctly rounded
+// one), 5 instructions instead of the 11 of a division (32768 tokens, 4 heads: 29.6 -> 24.5 us with the maxima by DPP). Exact where no remainder
+// underflows: at scales below 2^-80, where a remainder that counts could, and above 2^80 the division itself is taken.
+struct Ratio {
+  float scale, y;
+  bool direct;
+};
+__device__ __forceinline__ Ratio ratio_of(float scale) {
+  return Ratio{scale, div_rn(1.0f, scale), !(scale >= 0x1p-80f && scale <= 0x1p80f)};
+}
+// t = fl(x / scale), clamped
+template <int kFmt, bool kDirect>
+__device__ __forceinline__ float q8_ratio(float x, const Ratio& r) {
   constexpr float top = kFmt == OKVQ_Q8_INT8 ? 127.0f : 448.0f;
-  return fminf(fmaxf(div_rn(x, scale), -top), top);
+  float t;
+  if constexpr (kDirect) {
+    t = div_rn(x, r.scale);
+  } else {
+    const float q0 = x * r.y, q1 = __builtin_fmaf(__builtin_fmaf(-r.scale, q0, x), r.y, q0);
+    t = __builtin_fmaf(__builtin_fmaf(-r.scale, q1, x), r.y, q1);
+    if constexpr (kFmt == OKVQ_Q8_E4M3) t = __builtin_copysignf(t, x);  // -0 has a code, and its remainder is +0
+  }
+  return fminf(fmaxf(t, -top), top);
 }
 // codes of four ratios as the bytes of a dword
 template <int kFmt>
@@ -71,11 +93,8 @@ __global__ __launch_bounds__(kThreads) void k_q8_append(Q8AppendArgs p) {
     va = fmaxf(va, fmaxf(fmaxf(fabsf(row_lo<kBf16>(vr[i].x)), fabsf(row_hi<kBf16>(vr[i].x))),
                          fmaxf(fabsf(row_lo<kBf16>(vr[i].y)), fabsf(row_hi<kBf16>(vr[i].y)))));
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    ka = fmaxf(ka, __shfl_xor(ka, d));
-    va = fmaxf(va, __shfl_xor(va, d));
-  }
+  ka = wave_max(ka);
+  va = wave_max(va);
   if ((tid & 63) == 0) {
     amax_k[wave] = ka;
     amax_v[wave] = va;
@@ -105,22 +124,29 @@ __global__ __launch_bounds__(kThreads) void k_q8_append(Q8AppendArgs p) {
 
   const int64_t slot = q8_slot(q8_page(c.table + (int64_t)b * c.max_pages, block, c), h, block, c);
   uint32_t* kd = reinterpret_cast<uint32_t*>(c.k_codes + slot * kQ8Block) + cg;
-  float vq[4][4];  // [channel][token]
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    kd[(4 * tg + i) * 32] = q8_pack<kFmt>(q8_ratio<kFmt>(row_lo<kBf16>(kr[i].x), sk), q8_ratio<kFmt>(row_hi<kBf16>(kr[i].x), sk),
-                                          q8_ratio<kFmt>(row_lo<kBf16>(kr[i].y), sk), q8_ratio<kFmt>(row_hi<kBf16>(kr[i].y), sk));
-    vq[0][i] = q8_ratio<kFmt>(row_lo<kBf16>(vr[i].x), sv);
-    vq[1][i] = q8_ratio<kFmt>(row_hi<kBf16>(vr[i].x), sv);
-    vq[2][i] = q8_ratio<kFmt>(row_lo<kBf16>(vr[i].y), sv);
-    vq[3][i] = q8_ratio<kFmt>(row_hi<kBf16>(vr[i].y), sv);
-  }
   // Slot 64 j + 16 g + n of the block is kept at n ^ j within its row of 16: lanes that differ in j alone
   // would otherwise meet in one bank
   const int j = cg >> 3, bb = (cg >> 2) & 1, n0 = (cg & 3) * 4, a = tg >> 2, g = tg & 3;
+  const Ratio rk = ratio_of(sk), rv = ratio_of(sv);
+  auto code = [&](auto direct) {
+    constexpr bool kDirect = decltype(direct)::value;
+    float vq[4][4];  // [channel][token]
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    vt[((64 * j + 16 * g + ((n0 + e) ^ j)) << 2) + 2 * bb + a] = q8_pack<kFmt>(vq[e][0], vq[e][1], vq[e][2], vq[e][3]);
+    for (int i = 0; i < 4; ++i) {
+      kd[(4 * tg + i) * 32] =
+          q8_pack<kFmt>(q8_ratio<kFmt, kDirect>(row_lo<kBf16>(kr[i].x), rk), q8_ratio<kFmt, kDirect>(row_hi<kBf16>(kr[i].x), rk),
+                        q8_ratio<kFmt, kDirect>(row_lo<kBf16>(kr[i].y), rk), q8_ratio<kFmt, kDirect>(row_hi<kBf16>(kr[i].y), rk));
+      vq[0][i] = q8_ratio<kFmt, kDirect>(row_lo<kBf16>(vr[i].x), rv);
+      vq[1][i] = q8_ratio<kFmt, kDirect>(row_hi<kBf16>(vr[i].x), rv);
+      vq[2][i] = q8_ratio<kFmt, kDirect>(row_lo<kBf16>(vr[i].y), rv);
+      vq[3][i] = q8_ratio<kFmt, kDirect>(row_hi<kBf16>(vr[i].y), rv);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      vt[((64 * j + 16 * g + ((n0 + e) ^ j)) << 2) + 2 * bb + a] = q8_pack<kFmt>(vq[e][0], vq[e][1], vq[e][2], vq[e][3]);
+  };
+  if (kBf16 && (rk.direct || rv.direct)) code(std::true_type{});  // fp16 rows have scales of 2^-33 to 2^9
+  else code(std::false_type{});
   __syncthreads();
   reinterpret_cast<uint4*>(c.v_codes + slot * kQ8Block)[tid] =
       reinterpret_cast<const uint4*>(vt)[(tid & ~15) | ((tid & 15) ^ (tid >> 6))];
