@@ -113,18 +113,16 @@ template <bool kBf16>
 __device__ __forceinline__ float row_hi(uint32_t w) {
   return kBf16 ? __builtin_bit_cast(float, w & 0xffff0000u) : h2f(w >> 16);
 }
-// fp32 -> bfloat16 bits, round to nearest even (finite values, or infinities, which stay)
-__device__ __forceinline__ uint32_t f2bf(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
-}
-template <bool kBf16>
-__device__ __forceinline__ uint32_t row_bits(float x) {
-  return kBf16 ? f2bf(x) : f2h(x);
-}
+// two fp32 values rounded to nearest even into a dword
 template <bool kBf16>
 __device__ __forceinline__ uint32_t row_pack(float lo, float hi) {
-  return row_bits<kBf16>(lo) | (row_bits<kBf16>(hi) << 16);
+  if constexpr (kBf16) {
+    typedef float float2v __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(float2v{lo, hi}, bf2v));
+  } else {
+    return f2h(lo) | (f2h(hi) << 16);
+  }
 }
 
 // A load from a wave-uniform address through the scalar cache: for what earlier launches wrote and this one only
