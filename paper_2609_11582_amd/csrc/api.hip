@@ -40,7 +40,7 @@ okvq_status scratch_address(void** out) {
   return OKVQ_OK;
 }
 
-constexpr int32_t kVersion = 600;  // 0.6.0: bit-width ladder (b-bit keys and values)
+constexpr int32_t kVersion = 700;  // 0.7.0: rotary positions, paged 8-bit cache
 
 // ---- fixed Gaussian codebook (Sec. 2.1, Eq. 3): Lloyd-Max quantizer of N(0, 1), 4 levels ----
 double phi(double x) { return std::isinf(x) ? 0.0 : std::exp(-0.5 * x * x) / std::sqrt(2.0 * M_PI); }

@@ -158,7 +158,7 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
     if positions.shape != (B, 3, n):
         raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
     st = lib().okvq_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, pos, None if lens is None else _ints(lens, B, "lens"),
-                           oq, ok, _ROW_TYPES[dt], flags, _stream(stream))
+                           oq, ok, _ROW_TYPES[dt], int(flags), _stream(stream))
     if check and st:
         _check(st, "okvq_rotary")
     return st
@@ -223,9 +223,9 @@ def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, 
     """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128]) into one layer's pages, after
     okvq_q8_extend; lens: the lengths with them."""
     B, H, _ = cache._sizes
-    dev, dt = _device(), cache.row_dtype
+    dev, dt, n_max = _device(), cache.row_dtype, int(n_max)
     nbytes = B * H * n_max * 256
-    st = lib().okvq_q8_append(_cache_ref(cache, dev), layer, _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
+    st = lib().okvq_q8_append(_cache_ref(cache, dev), int(layer), _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
                               _need(v_new, nbytes, dt, "v_new", dev), _ints(n_new, B, "n_new"),
                               _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, _stream(stream))
     if check and st:
@@ -248,12 +248,12 @@ def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, s
     """Attention of rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
     tokens of each sequence, causal, or OKVQ_Q8_CROSS. lens: the lengths with the new tokens."""
     B, _, Hq = cache._sizes
-    dev, dt = _device(), cache.row_dtype
+    dev, dt, n_max = _device(), cache.row_dtype, int(n_max)
     nbytes = B * Hq * n_max * 256
-    st = lib().okvq_q8_attention(_cache_ref(cache, dev), layer, _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
-                                 _ints(n_new, B, "n_new"), _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, sm_scale,
+    st = lib().okvq_q8_attention(_cache_ref(cache, dev), int(layer), _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
+                                 _ints(n_new, B, "n_new"), _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, float(sm_scale),
                                  _need(out, nbytes, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
-                                 flags, _stream(stream))
+                                 int(flags), _stream(stream))
     if check and st:
         _check(st, "okvq_q8_attention")
     return st

@@ -611,3 +611,80 @@ def test_blocks_of_zero_values(fmt, n_q):
         r = np.abs(out[0, j].double().cpu().numpy() - ref) / bound
         _say(f"zero blocks {fmt} rows {n_q} head {j}: worst err / bound {r.max():.3f}")
         assert r.max() <= 1
+
+
+@pytest.mark.parametrize("n_q", [1, 30])
+def test_pool_beyond_32_bits(n_q):
+    """Pages whose codes lie past 2^32 bytes of a pool, in the second layer, against the same rows in a small cache."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    H, Hq, P, n = 8, 16, 9000, 700
+    k, v, q = _rows(101, 1, H, n, 128), _rows(102, 1, H, n, 128), _rows(103, 1, Hq, n_q, 128)
+    outs = []
+    for pages, layers in ((P, 2), (20, 1)):
+        c = okvq.Q8Cache(1, H, Hq, pages, 4, layers=layers, page_tokens=256)
+        c["block_table"][0, :3] = _i32([pages - 1, pages - 3, pages - 2])
+        _append(c, layers - 1, k, v, [0], [n])
+        outs.append((_attend(c, [n], q, [n_q], layer=layers - 1), c["k_codes"][-1, -1].clone(), c["v_codes"][-1, -3].clone()))
+    assert 2 * P * H * 256 * 128 > 1 << 32 and (P - 1) * H * 256 * 128 * 2 > 1 << 32
+    assert all(torch.equal(x, y) for x, y in zip(*outs))
+
+
+def test_two_graphs_and_two_streams():
+    """Two captured steps with workspaces of their own, replayed on two streams at once, several times."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B, H, Hq, lens = 2, 2, 14, [5000, 3000]
+    sides, want = [], []
+    for i in range(2):
+        c = _filled(B, H, Hq, lens, 64, "int8", "fp16", 110 + i)
+        q = _rows(120 + i, B, Hq, 1 + 20 * i, 128).cuda()
+        n = q.shape[2]
+        want.append(_attend(c, lens, q, [n] * B))
+        out, ws, new = torch.zeros_like(q), okvq.q8_workspace(c.dims, 5000, n), _i32([n] * B)
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            okvq.okvq_q8_attention(c, 0, lens, q, [n] * B, new, n, SM, out, ws)
+        sides.append((stream, graph, out, c, q, ws, new))
+    for t in range(5):
+        for _, _, out, *_ in sides:
+            out.fill_(t)
+        torch.cuda.synchronize()
+        for stream, graph, *_ in sides:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (_, _, out, *_), ref in zip(sides, want):
+            assert torch.equal(out, ref), t
+
+
+def test_lengths_on_the_device_rule():
+    """Host lengths only plan: a plan for shorter, longer or empty sequences gives the same rows up to the roundings of
+    another number of splits."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    lens = [2500, 900, 1]
+    c = _filled(3, 1, 4, lens, 64, "int8", "fp16", 130)
+    for n in (1, 24):
+        q = _rows(131, 3, 4, n, 128)
+        new, nd = [min(n, m) for m in lens], _i32([min(n, m) for m in lens])
+        ws = okvq.q8_workspace(c.dims, 2560, n)
+        for plan in ([0, 0, 0], [2560, 2560, 2560], [100, 1, 2000]):
+            out = torch.full(q.shape, 9.0, dtype=torch.float16, device="cuda")
+            okvq.okvq_q8_attention(c, 0, plan, q.cuda(), new, nd, n, SM, out, ws)
+            _check_attention(c, out, lens, q, new, "int8", "fp16", f"planned as {plan}, rows {n}")
+
+
+def test_counts_of_numpy():
+    import paper_2609_11582_amd as okvq
+    c = okvq.Q8Cache(2, 1, 1, 10, 4)
+    k = _rows(140, 2, 1, 33, 128)
+    lens = np.array([33, 20], np.int64)
+    c["block_table"][:, 0] = _i32([3, 4])
+    c["seq_lens"].copy_(_i32(lens.tolist()))
+    okvq.okvq_q8_append(c, np.int64(0), lens, k.cuda(), k.cuda(), np.array([33, 20]), _i32([33, 20]), np.int32(33))
+    _check_bytes(_numpy(c), k, k, [33, 20], "int8")
