@@ -10,7 +10,7 @@ namespace okvq {
 constexpr int kQ8Block = kW * kD;  // bytes of one block of codes: 32 tokens x 128 channels
 constexpr int kQ8MaxBatch = 1024;  // slots: one thread each in the page kernels
 constexpr int kQ8Cols = 16;        // query columns of a tile of the split kernel
-constexpr int kQ8PromptCols = 256; // and of the prompt kernel
+constexpr int kQ8PromptCols = 256; // and of the prompt kernel at most
 
 // ---- rotary --------------------------------------------------------------------------------------
 struct RotaryArgs {
@@ -72,7 +72,7 @@ struct Q8Plan {
 };
 void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens);
 size_t q8_workspace_bound(int G, int n_max);  // split records of every call of up to n_max rows
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, int most, int format, int dtype, int B, hipStream_t s);
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
 hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
 
 // Page calls, on the whole cache

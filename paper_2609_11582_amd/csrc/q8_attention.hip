@@ -270,17 +270,22 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 //   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
 //   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
+// * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
+//   a token (prompts x 28 heads: 64 tokens 12.2 -> 9.3 us, 512 26.0 -> 22.0, 2048 78 -> 72.5; 512 rows against 32768 tokens 322
+//   -> 485, as every work-group widens all codes). Up to 128 rows the second half of the waves only brings tiles, which is
+//   as good (16 tokens 8.4 us, in halves 9.1).
 // * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
 //   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
 void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
   const int64_t rows = (int64_t)n_max * G;
   const bool few = rows <= kQ8Cols;
-  p.cols = few ? kQ8Cols : kQ8PromptCols;
+  int longest = 0;
+  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
+  const bool half = rows > 128 && longest <= 2048 && B * H * ((rows + 255) / 256) <= 256;
+  p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
   p.rows = (int)std::min<int64_t>(rows, p.cols);
   const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
-  int longest = 0;
-  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
   const int64_t round = few ? kW * kWaves : longest < 4096 ? 512 : 256;  // tokens of a round
   const int64_t units = (int64_t)H * p.ntile;
   const auto fits = [&](int64_t rounds) {
@@ -326,8 +331,8 @@ hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int
   a.splits = p.splits;
   const bool bf16 = dtype == OKVQ_BF16;
   hipError_t e;
-  if (p.cols == kQ8PromptCols) {
-    e = launch_q8_prompt(a, p.most, format, dtype, B, s);
+  if (p.cols != kQ8Cols) {
+    e = launch_q8_prompt(a, p, format, dtype, B, s);
   } else {
     const dim3 grid(p.most, a.c.H, B), block(kThreads);
     if (format == OKVQ_Q8_INT8) {

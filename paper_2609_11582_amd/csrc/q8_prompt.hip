@@ -21,20 +21,19 @@
 namespace okvq {
 namespace {
 
-constexpr int kWaves = 8;
-constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 64;                 // tokens
 constexpr int kOperand = 64;              // 16-byte slots of a matrix operand
-static_assert(kQ8PromptCols == 32 * kWaves, "32 columns a wave");
 
-struct Raw {                              // a thread's 16 bytes of keys or of values, and the block's scale
-  uint4 x;
-  float scale;
-  uint32_t keep;
+template <int kPieces>
+struct Raw {                              // a thread's 16 bytes of keys or of values of kPieces blocks, and the blocks' scales
+  uint4 x[kPieces];
+  float scale[kPieces];
+  uint32_t keep[kPieces];
 };
 
-template <int kFmt, bool kBf16>
-__global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
+template <int kFmt, bool kBf16, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, int B) {
+  constexpr int kCols = 32 * kWaves, kPieces = 8 / kWaves;
   // two buffers of keys [block][16 channels][half h, token: at token ^ (channels & 7)] and of values
   // [block][32 channels][step s][half h, channel], as operands; the scales of three tiles, as the keys are ahead
   __shared__ uint4 kbuf[2][2][8][kOperand], vbuf[2][2][4][2][kOperand];
@@ -50,9 +49,9 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + (int64_t)b * c.max_pages;
   const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
-  const int r0 = tile * kQ8PromptCols, i_first = r0 / p.G;
+  const int r0 = tile * kCols, i_first = r0 / p.G;
   if (i_first >= n) return;
-  const int i_last = min((r0 + kQ8PromptCols - 1) / p.G, n - 1);
+  const int i_last = min((r0 + kCols - 1) / p.G, n - 1);
   const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
   // the wave's columns, and the tokens that they see
   const int r = r0 + 32 * wave + col, i = r / p.G, hq = h * p.G + (r - i * p.G);
@@ -64,31 +63,42 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   const int ntile = (vis_last + kTile - 1) / kTile;
   const int per = (ntile + nsplit - 1) / nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
 
-  // staging: thread tid has 16 bytes of key row tid / 8 and value slot tid % 256 of block tid / 256
-  const int sb = wave >> 2, krow = (tid >> 3) & 31, kchunk = tid & 7, vslot = tid & 255;
+  // Staging: a thread has 16 bytes of key row tid / 8 % 32 and of value slot tid % 256 of kPieces of the tile's two blocks.
   // A block that lies behind the sequence is read from some page of the pool, and zeroed on its way to LDS: what a zero
   // weight multiplies has to be finite. Values of a subnormal scale count as zero too: their logarithm is none.
-  auto load = [&](int t, const uint8_t* codes, const float* scales, float least, Raw& r) {
-    const int block = 2 * t + sb;
-    const int64_t slot = q8_slot(q8_page(table, block, c), h, block, c);
-    r.x = *reinterpret_cast<const uint4*>(codes + slot * kQ8Block + vslot * 16);
-    r.scale = uniform_load(scales + slot);
-    r.keep = block * kW < len && r.scale >= least ? ~0u : 0u;
-    r.scale = r.keep ? r.scale : 1.0f;
+  const int sb = kPieces == 2 ? 0 : wave >> 2, krow = (tid >> 3) & 31, kchunk = tid & 7, vslot = tid & 255;
+  auto load = [&](int t, const uint8_t* codes, const float* scales, float least, Raw<kPieces>& r) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int block = 2 * t + sb + e;
+      const int64_t slot = q8_slot(q8_page(table, block, c), h, block, c);
+      r.x[e] = *reinterpret_cast<const uint4*>(codes + slot * kQ8Block + vslot * 16);
+      const float scale = uniform_load(scales + slot);
+      r.keep[e] = block * kW < len && scale >= least ? ~0u : 0u;
+      r.scale[e] = r.keep[e] ? scale : 1.0f;
+    }
   };
-  auto load_keys = [&](int t, Raw& r) { load(t, c.k_codes, c.k_scale, 0.0f, r); };
-  auto load_values = [&](int t, Raw& r) { load(t, c.v_codes, c.v_scale, 0x1p-126f, r); };
-  auto store_keys = [&](int u, const Raw& r) {
+  auto load_keys = [&](int t, Raw<kPieces>& r) { load(t, c.k_codes, c.k_scale, 0.0f, r); };
+  auto load_values = [&](int t, Raw<kPieces>& r) { load(t, c.v_codes, c.v_scale, 0x1p-126f, r); };
+  auto store_keys = [&](int u, const Raw<kPieces>& r) {
     const int kp = krow ^ kchunk;
-    kbuf[u & 1][sb][kchunk][kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.x & r.keep, r.x.y & r.keep));
-    kbuf[u & 1][sb][kchunk][32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.z & r.keep, r.x.w & r.keep));
-    kscale[u % 3][sb] = r.scale;  // every lane writes the same
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      uint4* to = kbuf[u & 1][sb + e][kchunk];
+      to[kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x & r.keep[e], r.x[e].y & r.keep[e]));
+      to[32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z & r.keep[e], r.x[e].w & r.keep[e]));
+      kscale[u % 3][sb + e] = r.scale[e];  // every lane writes the same
+    }
   };
-  auto store_values = [&](int u, const Raw& r) {
+  auto store_values = [&](int u, const Raw<kPieces>& r) {
     const int j = vslot >> 6, g = (vslot >> 4) & 3, ch = vslot & 15;
-    vbuf[u & 1][sb][j][g >> 1][32 * (g & 1) + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.x & r.keep, r.x.y & r.keep));
-    vbuf[u & 1][sb][j][g >> 1][32 * (g & 1) + 16 + ch] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x.z & r.keep, r.x.w & r.keep));
-    vscale[u & 1][sb] = r.scale;
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      uint4* to = vbuf[u & 1][sb + e][j][g >> 1] + 32 * (g & 1) + ch;
+      to[0] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x & r.keep[e], r.x[e].y & r.keep[e]));
+      to[16] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z & r.keep[e], r.x[e].w & r.keep[e]));
+      vscale[u & 1][sb + e] = r.scale[e];
+    }
   };
 
   // query operands: column's channels 16 kk + 8 half .. + 7
@@ -119,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
   // The loop runs the next tile's scores beside this tile's softmax: matrix and vector instructions of one wave overlap
   // where they do not depend on each other. So the keys in LDS are a tile ahead of the values.
   const int nt = t_end - t_begin;
-  Raw kr, vr;
+  Raw<kPieces> kr, vr;
   floatx16 s[2], s2[2];
   float top[2] = {kNoScore, kNoScore};  // largest dot of each block of s
   auto scores = [&](const uint4 (&k)[2][8][kOperand], floatx16 (&d)[2]) {
@@ -264,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
                                                                      row_pack<kBf16>(acc[j][e + 2] * f, acc[j][e + 3] * f));
     return;
   }
-  float* rec = p.ws + ((int64_t)first * c.H * p.ntile + ((int64_t)h * p.ntile + tile) * nsplit + split) * (kQ8PromptCols * (kD + 4));
+  float* rec = p.ws + ((int64_t)first * c.H * p.ntile + ((int64_t)h * p.ntile + tile) * nsplit + split) * (kCols * (kD + 4));
   const int cc = 32 * wave + col;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -272,20 +282,21 @@ __global__ __launch_bounds__(kThreads) void k_q8_prompt(Q8AttendArgs p, int B) {
     for (int e = 0; e < 16; e += 4)
       *reinterpret_cast<floatx4*>(rec + cc * kD + 32 * j + 2 * e + 4 * half) =
           floatx4{acc[j][e], acc[j][e + 1], acc[j][e + 2], acc[j][e + 3]};
-  if (half == 0) *reinterpret_cast<floatx4*>(rec + kQ8PromptCols * kD + 4 * cc) = floatx4{M, m, l, 0.0f};
+  if (half == 0) *reinterpret_cast<floatx4*>(rec + kCols * kD + 4 * cc) = floatx4{M, m, l, 0.0f};
 }
 
 }  // namespace
 
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, int most, int format, int dtype, int B, hipStream_t s) {
-  const dim3 grid((unsigned)(B * a.c.H * a.ntile), most), block(kThreads);
-  if (format == OKVQ_Q8_INT8) {
-    if (dtype == OKVQ_BF16) hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_INT8, true>), grid, block, 0, s, a, B);
-    else hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_INT8, false>), grid, block, 0, s, a, B);
-  } else {
-    if (dtype == OKVQ_BF16) hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_E4M3, true>), grid, block, 0, s, a, B);
-    else hipLaunchKernelGGL((k_q8_prompt<OKVQ_Q8_E4M3, false>), grid, block, 0, s, a, B);
-  }
+template <int kFmt, bool kBf16>
+static void launch(const Q8AttendArgs& a, const Q8Plan& p, int B, hipStream_t s) {
+  const dim3 grid((unsigned)(B * a.c.H * p.ntile), p.most);
+  if (p.cols == 256) hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 8>), grid, dim3(512), 0, s, a, B);
+  else hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 4>), grid, dim3(256), 0, s, a, B);
+}
+
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
+  if (format == OKVQ_Q8_INT8) dtype == OKVQ_BF16 ? launch<OKVQ_Q8_INT8, true>(a, p, B, s) : launch<OKVQ_Q8_INT8, false>(a, p, B, s);
+  else dtype == OKVQ_BF16 ? launch<OKVQ_Q8_E4M3, true>(a, p, B, s) : launch<OKVQ_Q8_E4M3, false>(a, p, B, s);
   return hipGetLastError();
 }
 
