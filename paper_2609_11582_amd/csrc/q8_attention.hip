@@ -210,6 +210,15 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   if ((tid & 31) == 0) *reinterpret_cast<floatx4*>(rec + kQ8Cols * kD + 4 * cc) = floatx4{Mt, mt, lt, 0.0f};
 }
 
+// op over the 32 lanes of a half wave, in every lane of it
+template <typename Op>
+__device__ __forceinline__ float half_reduce(float v, Op&& op) {
+  v = op(v, fdpp<0xB1>(v));
+  v = op(v, fdpp<0x4E>(v));
+  v = op(v, fswap4(v));
+  v = op(v, fswap8(v));
+  return op(v, fswap16(v));
+}
 // Join the splits: kGroups groups of 32 lanes share a column's (a group takes every kGroups-th split, then the
 // groups are added), kCols columns a work-group
 template <bool kBf16, int kGroups, int kCols>
@@ -228,28 +237,38 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
   floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   float scale = 0.0f;
   if (live) {
-    // every group forms the references and the sum of all splits (a lane takes every 32nd), and its own factors
+    // A group has 8 splits at most: their sums are on their way while the references and the softmax sum of all splits
+    // are formed, which every group does for itself (a lane takes every 32nd split)
     const float* stat = rec + cols * kD + 4 * cc;
-    float M = kNoScore, m = kNoScore, l = 0.0f;
-    for (int s = lane; s < nsplit; s += 32) {
-      const floatx4 st = *reinterpret_cast<const floatx4*>(stat + (int64_t)s * recf);
-      const float m2 = fmaxf(m, st[1]);
-      l = l * __builtin_amdgcn_exp2f(m - m2) + st[2] * __builtin_amdgcn_exp2f(st[1] - m2);
-      m = m2;
-      M = fmaxf(M, st[0]);
-    }
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const float m1 = __shfl_xor(m, d), l1 = __shfl_xor(l, d), m2 = fmaxf(m, m1);
-      l = l * __builtin_amdgcn_exp2f(m - m2) + l1 * __builtin_amdgcn_exp2f(m1 - m2);
-      m = m2;
-      M = fmaxf(M, __shfl_xor(M, d));
-    }
-    scale = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
     const float* sums = rec + cc * kD + 4 * lane;
-#pragma unroll 4
-    for (int s = grp; s < nsplit; s += kGroups)
-      o += *reinterpret_cast<const floatx4*>(sums + (int64_t)s * recf) * __builtin_amdgcn_exp2f(stat[(int64_t)s * recf] - M);
+    floatx4 v[8];
+    float vM[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t at = (int64_t)min(grp + k * kGroups, nsplit - 1) * recf;
+      v[k] = *reinterpret_cast<const floatx4*>(sums + at);
+      vM[k] = stat[at];
+    }
+    constexpr int kStats = (8 * kGroups + 31) / 32;
+    floatx4 st[kStats];
+    float M = kNoScore, m = kNoScore, l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kStats; ++k) {
+      const int s = lane + 32 * k;
+      st[k] = *reinterpret_cast<const floatx4*>(stat + (int64_t)min(s, nsplit - 1) * recf);
+      if (s >= nsplit) st[k][2] = 0.0f;  // counted already
+      M = fmaxf(M, st[k][0]);
+      m = fmaxf(m, st[k][1]);
+    }
+    M = half_reduce(M, [](float a, float b) { return fmaxf(a, b); });
+    m = half_reduce(m, [](float a, float b) { return fmaxf(a, b); });
+#pragma unroll
+    for (int k = 0; k < kStats; ++k) l += st[k][2] * __builtin_amdgcn_exp2f(st[k][1] - m);
+    l = half_reduce(l, [](float a, float b) { return a + b; });
+    scale = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (grp + k * kGroups < nsplit) o += v[k] * __builtin_amdgcn_exp2f(vM[k] - M);
   }
   if constexpr (kGroups > 1) {
     part[tid >> 5][lane] = o;
@@ -296,6 +315,7 @@ void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
     return n * units <= groups;
   };
   int64_t lo = 1, hi = std::max<int64_t>((longest + round - 1) / round, 1);  // hi rounds: one split each
+  if (B * units > groups) lo = hi;
   while (lo < hi) {  // the fewest rounds that fit
     const int64_t mid = (lo + hi) / 2;
     if (fits(mid)) hi = mid;
