@@ -50,8 +50,8 @@ hipError_t launch_q8_append(const Q8AppendArgs& a, int format, int dtype, int B,
 
 // Splits of each sequence: sequence b has those from first[b] on, up to first[b + 1]; with none there it has one split,
 // which writes the output rows itself
-struct Q8Splits {
-  uint16_t first[kQ8MaxBatch + 1];
+struct __attribute__((aligned(4))) Q8Splits {
+  uint16_t first[kQ8MaxBatch + 2];  // (read as dwords)
 };
 struct Q8AttendArgs {
   Q8View c;
@@ -139,6 +139,14 @@ __device__ __forceinline__ int q8_page(const int32_t* row, int block, const Q8Vi
 // Index of (page, head, block within the page) among the blocks of a layer
 __device__ __forceinline__ int64_t q8_slot(int page, int h, int block, const Q8View& c) {
   return (((int64_t)page * c.H + h) << c.bshift) + (block & ((1 << c.bshift) - 1));
+}
+// first[b] and how many follow, b wave-uniform: two scalar dword loads
+__device__ __forceinline__ int q8_splits(const Q8Splits& s, int b, int* records) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(s.first);
+  const uint32_t lo = w[b >> 1], hi = w[(b + 1) >> 1];
+  const int first = (b & 1) ? lo >> 16 : lo & 0xffffu, next = (b & 1) ? hi & 0xffffu : hi >> 16;
+  *records = next - first;
+  return first;
 }
 __device__ __forceinline__ int q8_len(const Q8View& c, int b) {
   return min(max(uniform_load(c.lens + b), 0), c.max_pages << (c.bshift + 5));

@@ -66,25 +66,25 @@ __global__ __launch_bounds__(kThreads) void k_q8_append(Q8AppendArgs p) {
   const int len = q8_len(c, b), n = min(min(max(p.n_new[b], 0), p.n_max), len), old = len - n;
   const int first = old / kW, block = first + (int)blockIdx.x, t0 = block * kW;
   if (n == 0 || t0 >= len) return;
+  const int64_t slot = q8_slot(q8_page(c.table + (int64_t)b * c.max_pages, block, c), h, block, c);
   const int cg = tid & 31, tg = tid >> 5;
   const int64_t head = (int64_t)b * c.H + h;
   const uint2* kn = reinterpret_cast<const uint2*>(p.k) + head * p.n_max * 32 + cg;
   const uint2* vn = reinterpret_cast<const uint2*>(p.v) + head * p.n_max * 32 + cg;
   const uint2* ks = reinterpret_cast<const uint2*>(c.k_stage) + head * kW * 32 + cg;
   const uint2* vs = reinterpret_cast<const uint2*>(c.v_stage) + head * kW * 32 + cg;
+  // every row from where it is, without a branch; rows behind the last token from its address, and zeroed
   uint2 kr[4], vr[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = 4 * tg + i, t = t0 + row;
-    kr[i] = vr[i] = make_uint2(0u, 0u);
-    if (t < old) {
-      kr[i] = ks[row * 32];
-      vr[i] = vs[row * 32];
-    } else if (t < len) {
-      kr[i] = kn[(int64_t)(t - old) * 32];
-      vr[i] = vn[(int64_t)(t - old) * 32];
-    }
+    const int64_t at = (int64_t)min(t - old, n - 1) * 32;
+    kr[i] = *(t < old ? ks + row * 32 : kn + at);
+    vr[i] = *(t < old ? vs + row * 32 : vn + at);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t0 + 4 * tg + i >= len) kr[i] = vr[i] = make_uint2(0u, 0u);
   float ka = 0.0f, va = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -122,7 +122,6 @@ __global__ __launch_bounds__(kThreads) void k_q8_append(Q8AppendArgs p) {
     }
   }
 
-  const int64_t slot = q8_slot(q8_page(c.table + (int64_t)b * c.max_pages, block, c), h, block, c);
   uint32_t* kd = reinterpret_cast<uint32_t*>(c.k_codes + slot * kQ8Block) + cg;
   // Slot 64 j + 16 g + n of the block is kept at n ^ j within its row of 16: lanes that differ in j alone
   // would otherwise meet in one bank

@@ -39,7 +39,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __shared__ float wM[kWaves][kQ8Cols], wm[kWaves][kQ8Cols], wl[kWaves][kQ8Cols];
   const Q8View& c = p.c;
   const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int first = p.splits.first[b], records = p.splits.first[b + 1] - first, nsplit = max(records, 1);
+  int records;
+  const int first = q8_splits(p.splits, b, &records), nsplit = max(records, 1);
   if (split >= nsplit) return;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -47,6 +48,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   const int stride = nsplit * kWaves;
   int block = split * kWaves + wave;
 
+  // The query rows, column's channels 64 (kk / 2) + 16 g + 8 (kk % 2) .. + 7, of rows that may not be live
+  const int i = col / p.G, hq = h * p.G + (col - i * p.G);
+  uint4 raw[4];
+  {
+    const uint4* q = reinterpret_cast<const uint4*>(p.q) + (((int64_t)b * c.Hq + min(hq, c.Hq - 1)) * p.n_max + min(i, p.n_max - 1)) * 16;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) raw[kk] = q[8 * (kk >> 1) + 2 * g + (kk & 1)];
+  }
   // A block's registers: key rows 16 tb + col (channels 16 g .. + 15 and 64 + 16 g .. + 15), value slots 64 j + lane,
   // and the scales, which are wave-uniform. Every address is inside the pool, so the first block is loaded before
   // the lengths say whether it is needed
@@ -72,30 +81,23 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   load_keys(slot);
   load_values(slot);
   int page = q8_page(row, block + stride, c);  // of the wave's next block
+  __asm__ volatile("" ::: "memory");           // the loads above go out before the length is waited for
 
   const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   if (n == 0) return;
   const int i_last = min((kQ8Cols - 1) / p.G, n - 1);
   const int vis_first = p.cross ? len : max(len - n + 1, 0);  // tokens that the first and the last row see
   const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
-  const int i = col / p.G, hq = h * p.G + (col - i * p.G);
   const bool live = i < n;
   const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
   const int nblk = (vis_last + kW - 1) / kW;
 
-  // query operands: column's channels 64 (kk / 2) + 16 g + 8 (kk % 2) .. + 7
   half8 qop[4];
   float qs = p.qscale;
-  {
-    const uint4* q = reinterpret_cast<const uint4*>(p.q) + (live ? ((int64_t)b * c.Hq + hq) * p.n_max + i : 0) * 16;
-    uint4 raw[4];
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      raw[kk] = q[8 * (kk >> 1) + 2 * g + (kk & 1)];
-      if (!live) raw[kk] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    qs *= query_operands<kBf16>(raw, qop, [](float v) { return max32(max16(v)); });
-  }
+  for (int kk = 0; kk < 4; ++kk)
+    if (!live) raw[kk] = make_uint4(0u, 0u, 0u, 0u);
+  qs *= query_operands<kBf16>(raw, qop, [](float v) { return max32(max16(v)); });
 
   float m = kNoScore, M = kNoScore, l = 0.0f;
   floatx4 acc[8];  // channel 16 t + 4 g + i of the column
@@ -226,7 +228,8 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
   __shared__ __attribute__((aligned(16))) floatx4 part[kGroups * kCols][32];
   const int h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, grp = (tid >> 5) % kGroups, cc = blockIdx.x * kCols + (tid >> 5) / kGroups;
-  const int first = p.splits.first[b], nsplit = p.splits.first[b + 1] - first;
+  int nsplit;
+  const int first = q8_splits(p.splits, b, &nsplit);
   if (nsplit == 0) return;
   const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int r = tile * cols + cc, i = r / p.G, hq = h * p.G + (r - i * p.G);

@@ -43,7 +43,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   // which see most, start first
   const int units = B * c.H, unit = blockIdx.x % units, split = blockIdx.y;
   const int tile = p.ntile - 1 - (int)(blockIdx.x / units), b = unit / c.H, h = unit - b * c.H;
-  const int first = p.splits.first[b], records = p.splits.first[b + 1] - first, nsplit = max(records, 1);
+  int records;
+  const int first = q8_splits(p.splits, b, &records), nsplit = max(records, 1);
   if (split >= nsplit) return;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
