@@ -30,6 +30,7 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
+constexpr int kFewRows = 32;                      // rows of a head that always take the split kernel
 constexpr int kRecFloatsQ8 = kQ8Cols * (kD + 4);  // a split's record: [16][128] sums, then [16] of (M, m, l, 0)
 constexpr int kCombineRow = kD + 4;               // floats of a combine row: 16 rows of a column fall into all banks
 
@@ -38,7 +39,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __shared__ __attribute__((aligned(16))) float cmb[kWaves][kQ8Cols * kCombineRow];
   __shared__ float wM[kWaves][kQ8Cols], wm[kWaves][kQ8Cols], wl[kWaves][kQ8Cols];
   const Q8View& c = p.c;
-  const int split = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x, h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
+  const int r0 = tile * kQ8Cols;  // first row of the tile
   int records;
   const int first = q8_splits(p.splits, b, &records), nsplit = max(records, 1);
   if (split >= nsplit) return;
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   int block = split * kWaves + wave;
 
   // The query rows, column's channels 64 (kk / 2) + 16 g + 8 (kk % 2) .. + 7, of rows that may not be live
-  const int i = col / p.G, hq = h * p.G + (col - i * p.G);
+  const int i = (r0 + col) / p.G, hq = h * p.G + (r0 + col - i * p.G);
   uint4 raw[4];
   {
     const uint4* q = reinterpret_cast<const uint4*>(p.q) + (((int64_t)b * c.Hq + min(hq, c.Hq - 1)) * p.n_max + min(i, p.n_max - 1)) * 16;
@@ -84,9 +86,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __asm__ volatile("" ::: "memory");           // the loads above go out before the length is waited for
 
   const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
-  if (n == 0) return;
-  const int i_last = min((kQ8Cols - 1) / p.G, n - 1);
-  const int vis_first = p.cross ? len : max(len - n + 1, 0);  // tokens that the first and the last row see
+  const int i_first = r0 / p.G, i_last = min((r0 + kQ8Cols - 1) / p.G, n - 1);
+  if (i_first >= n) return;
+  const int vis_first = p.cross ? len : max(len - n + i_first + 1, 0);  // tokens that the first and the last row see
   const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
   const bool live = i < n;
   const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
@@ -186,7 +188,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __syncthreads();
   const int cc = tid >> 5, ch = (tid & 31) * 4;
   static_assert(kThreads == 32 * kQ8Cols, "32 lanes a column");
-  const int ci = cc / p.G, chq = h * p.G + (cc - ci * p.G);
+  const int ci = (r0 + cc) / p.G, chq = h * p.G + (r0 + cc - ci * p.G);
   if (ci >= n) return;
   float Mt = kNoScore, mt = kNoScore;
 #pragma unroll
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
         make_uint2(row_pack<kBf16>(o[0] * f, o[1] * f), row_pack<kBf16>(o[2] * f, o[3] * f));
     return;
   }
-  float* rec = p.ws + ((int64_t)first * c.H + h * nsplit + split) * kRecFloatsQ8;
+  float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit + split) * kRecFloatsQ8;
   *reinterpret_cast<floatx4*>(rec + cc * kD + ch) = o;
   if ((tid & 31) == 0) *reinterpret_cast<floatx4*>(rec + kQ8Cols * kD + 4 * cc) = floatx4{Mt, mt, lt, 0.0f};
 }
@@ -290,6 +292,9 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 
 // Every split takes the same number of tokens at most, the least that needs no more work-groups than fit the GPU at
 // once: a ragged batch is shared evenly (16 sequences of 8704 to 16384 tokens: 46 -> 41 us against as many splits for each).
+// * The split kernel, 16 columns at a time, up to 32 rows of a head, and up to 112 (7 tiles, each with a read of the cache)
+//   where tokens x heads x tiles are few: 3 positions x 7 heads at 2048 tokens 18.3 -> 9.2 us against the prompt kernel, at
+//   131072 53.5 -> 33.4, 4 positions of 16 sequences at 8192 52.5 -> 48.5; 16 positions at 2048 20.2 -> 10.3, at 32768 28.2 -> 33.0.
 // * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
 //   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
@@ -302,9 +307,13 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 //   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
 void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
   const int64_t rows = (int64_t)n_max * G;
-  const bool few = rows <= kQ8Cols;
   int longest = 0;
-  for (int b = 0; b < B; ++b) longest = std::max(longest, lens[b]);
+  int64_t tokens = 0;
+  for (int b = 0; b < B; ++b) {
+    longest = std::max(longest, lens[b]);
+    tokens += lens[b];
+  }
+  const bool few = rows <= kFewRows || (rows <= 112 && tokens * H * ((rows + kQ8Cols - 1) / kQ8Cols) <= 1 << 18);
   const bool half = rows > 128 && longest <= 2048 && B * H * ((rows + 255) / 256) <= 256;
   p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
@@ -340,7 +349,7 @@ void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
 // have one split and no record. Calls of few rows and of many count by themselves
 size_t q8_workspace_bound(int G, int n_max) {
   const size_t few = (size_t)kQ8Groups * kQ8Cols, many = (size_t)kQ8PromptGroups * kQ8PromptCols;
-  return ((int64_t)n_max * G > kQ8Cols ? std::max(few, many) : few) * (kD + 4) * sizeof(float);
+  return ((int64_t)n_max * G > kFewRows ? std::max(few, many) : few) * (kD + 4) * sizeof(float);
 }
 
 template <int kGroups, int kCols>
@@ -359,7 +368,7 @@ hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int
   if (p.cols != kQ8Cols) {
     e = launch_q8_prompt(a, p, format, dtype, B, s);
   } else {
-    const dim3 grid(p.most, a.c.H, B), block(kThreads);
+    const dim3 grid(p.most, a.c.H * p.ntile, B), block(kThreads);
     if (format == OKVQ_Q8_INT8) {
       if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
       else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
