@@ -25,10 +25,10 @@ constexpr int kTile = 64;                 // tokens
 constexpr int kOperand = 64;              // 16-byte slots of a matrix operand
 
 template <int kPieces>
-struct Raw {                              // a thread's 16 bytes of keys or of values of kPieces blocks, and the blocks' scales
-  uint4 x[kPieces];
+struct Raw {                              // a thread's 16 bytes of keys or of values of kPieces blocks, the blocks' scales,
+  uint4 x[kPieces];                       // and which blocks of which pages are next
   float scale[kPieces];
-  uint32_t keep[kPieces];
+  int block[kPieces], page[kPieces];
 };
 
 template <int kFmt, bool kBf16, int kWaves>
@@ -65,29 +65,47 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   const int per = (ntile + nsplit - 1) / nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
 
   // Staging: a thread has 16 bytes of key row tid / 8 % 32 and of value slot tid % 256 of kPieces of the tile's two blocks.
-  // A block that lies behind the sequence is read from some page of the pool, and zeroed on its way to LDS: what a zero
-  // weight multiplies has to be finite. Values of a subnormal scale count as zero too: their logarithm is none.
+  // Behind the sequence its last block stands for those to come: what a zero weight multiplies has to be finite. Values
+  // of a subnormal scale count as zero, as their logarithm is none.
+  // Page ids and scales come through the scalar cache, whose waits are waits for all LDS reads too: a page is fetched a
+  // tile before its codes, and what is fetched is waited for at the head of the loop, where nothing is in flight.
   const int sb = kPieces == 2 ? 0 : wave >> 2, krow = (tid >> 3) & 31, kchunk = tid & 7, vslot = tid & 255;
-  auto load = [&](int t, const uint8_t* codes, const float* scales, float least, Raw<kPieces>& r) {
+  const int last = max((len - 1) / kW, 0);
+  auto fetch_page = [&](int t, Raw<kPieces>& r) {
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
-      const int block = 2 * t + sb + e;
-      const int64_t slot = q8_slot(q8_page(table, block, c), h, block, c);
-      r.x[e] = *reinterpret_cast<const uint4*>(codes + slot * kQ8Block + vslot * 16);
-      const float scale = uniform_load(scales + slot);
-      r.keep[e] = block * kW < len && scale >= least ? ~0u : 0u;
-      r.scale[e] = r.keep[e] ? scale : 1.0f;
+      r.block[e] = min(2 * t + sb + e, last);
+      r.page[e] = uniform_load(table + min(r.block[e] >> c.bshift, c.max_pages - 1));
     }
   };
-  auto load_keys = [&](int t, Raw<kPieces>& r) { load(t, c.k_codes, c.k_scale, 0.0f, r); };
-  auto load_values = [&](int t, Raw<kPieces>& r) { load(t, c.v_codes, c.v_scale, 0x1p-126f, r); };
+  auto load = [&](const uint8_t* codes, const float* scales, Raw<kPieces>& r) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      const int64_t slot = q8_slot(min(max(r.page[e], 0), c.P - 1), h, r.block[e], c);
+      r.x[e] = *reinterpret_cast<const uint4*>(codes + slot * kQ8Block + vslot * 16);
+      r.scale[e] = uniform_load(scales + slot);
+    }
+  };
+  // codes of tile t, whose page is known, and the page of the tile after it
+  auto load_keys = [&](int t, Raw<kPieces>& r) {
+    load(c.k_codes, c.k_scale, r);
+    fetch_page(t + 1, r);
+  };
+  auto load_values = [&](int t, Raw<kPieces>& r) {
+    load(c.v_codes, c.v_scale, r);
+    fetch_page(t + 1, r);
+  };
+  auto fetched = [&](const Raw<kPieces>& r) {
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) __asm__ volatile("" ::"s"(r.page[e]), "s"(r.scale[e]));
+  };
   auto store_keys = [&](int u, const Raw<kPieces>& r) {
     const int kp = krow ^ kchunk;
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
       uint4* to = kbuf[u & 1][sb + e][kchunk];
-      to[kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x & r.keep[e], r.x[e].y & r.keep[e]));
-      to[32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z & r.keep[e], r.x[e].w & r.keep[e]));
+      to[kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x, r.x[e].y));
+      to[32 + kp] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z, r.x[e].w));
       kscale[u % 3][sb + e] = r.scale[e];  // every lane writes the same
     }
   };
@@ -96,9 +114,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
       uint4* to = vbuf[u & 1][sb + e][j][g >> 1] + 32 * (g & 1) + ch;
-      to[0] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x & r.keep[e], r.x[e].y & r.keep[e]));
-      to[16] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z & r.keep[e], r.x[e].w & r.keep[e]));
-      vscale[u & 1][sb + e] = r.scale[e];
+      const uint32_t keep = r.scale[e] >= 0x1p-126f ? ~0u : 0u;
+      to[0] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].x & keep, r.x[e].y & keep));
+      to[16] = __builtin_bit_cast(uint4, widen8<kFmt>(r.x[e].z & keep, r.x[e].w & keep));
+      vscale[u & 1][sb + e] = keep ? r.scale[e] : 1.0f;
     }
   };
 
@@ -154,6 +173,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
     }
   };
   if (nt > 0) {
+    fetch_page(t_begin, kr);
+    fetch_page(t_begin, vr);
     load_keys(t_begin, kr);
     load_values(t_begin, vr);
     store_keys(0, kr);
@@ -176,6 +197,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
     load_keys(t_begin + u + 3, kr);
   };
   for (int u = 0; u < nt; ++u) {
+    fetched(kr);
+    fetched(vr);
     if (!busy) {
       stage(u);
       __syncthreads();
