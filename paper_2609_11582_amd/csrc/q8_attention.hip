@@ -155,7 +155,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
       m = m2;
       M = M2;
     }
-    const float f = __builtin_amdgcn_exp2f(fminf(m - M + lv + kWeightExp, 100.0f));
+    // finite, so that a weight of zero stays zero; the bound is reached only by weights p below 2^-112
+    const float f = __builtin_amdgcn_exp2f(fminf(m - M + lv + kWeightExp, 127.0f));
     uint32_t w[4];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)

@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kTile = 64;                 // tokens
 constexpr int kOperand = 64;              // 16-byte slots of a matrix operand
+constexpr float kLeastWeight = -60.0f;    // log2 of the weight at the reference m; at most 2^(kLazy - 60), zero as fp16
 
 template <int kPieces>
 struct Raw {                              // a thread's 16 bytes of keys or of values of kPieces blocks, the blocks' scales,
@@ -249,8 +250,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
     }
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
-      off[tb] = dead[tb] ? -m : lv[tb] + kWeightExp - M;  // zero codes take any finite weight
-      gain[tb] = __builtin_amdgcn_exp2f(fminf(-off[tb] - m, 126.0f));
+      // zero codes take any finite weight. Values too small beside others for a weight in fp16 take one that is zero
+      // there and still adds to the sum in fp32 (without it, scales 2^110 apart lost their blocks' part of the sum)
+      off[tb] = dead[tb] ? -m : fmaxf(lv[tb] + kWeightExp - M, kLeastWeight - m);
+      gain[tb] = __builtin_amdgcn_exp2f(-off[tb] - m);
     }
     // One stretch without a branch: the next scores beside this tile's weights, then the value product beside the next
     // scores' maxima and the tiles to come on their way to LDS (behind the last tile they are some page's, and unused)

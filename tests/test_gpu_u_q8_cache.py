@@ -688,3 +688,73 @@ def test_counts_of_numpy():
     c["seq_lens"].copy_(_i32(lens.tolist()))
     okvq.okvq_q8_append(c, np.int64(0), lens, k.cuda(), k.cuda(), np.array([33, 20]), _i32([33, 20]), np.int32(33))
     _check_bytes(_numpy(c), k, k, [33, 20], "int8")
+
+
+@pytest.mark.parametrize("n_q", [1, 150])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_value_scales_far_apart(fmt, n_q):
+    """Blocks of bfloat16 values whose scales lie 2^150 apart share the attention: the small ones count in the softmax sum."""
+    import torch
+    n = 400
+    c = _new(1, 1, 2, [n], 64, fmt, "bf16")
+    large = (torch.arange(n) // 32 % 3 == 1)[:, None]
+    k = _rows(61, 1, 1, n, 128, dtype="bf16")
+    v = (torch.where(large, 2.0 ** 75, 2.0 ** -75) * _rows(62, 1, 1, n, 128).double()).to(torch.bfloat16)
+    _append(c, 0, k, v, [0], [n])
+    q = _rows(63, 1, 2, n_q, 128, dtype="bf16")
+    out = _attend(c, [n], q, [n_q])
+    a = _numpy(c)
+    kk, vv = oq.read_sequence(a, 0, 0, 0, n, fmt)
+    for j in range(2):
+        ref, bound = oq.attention(q[0, j].double().numpy(), kk, vv / 2.0 ** 75, n - n_q + np.arange(n_q) + 1, SM, HALF["bf16"])
+        r = np.abs(out[0, j].double().cpu().numpy() / 2.0 ** 75 - ref) / bound
+        _say(f"far scales {fmt} rows {n_q} head {j}: worst err / bound {r.max():.3f}")
+        assert r.max() <= 1
+
+
+@pytest.mark.parametrize("n_q", [1, 150])
+def test_small_weights_of_large_values(n_q):
+    """A block with weights of 2^-100 whose values are 2^180 times the others': its products are the largest by 2^80. It
+    is met by the wave that has the dominant block (every eighth is the same wave's), before it and after it."""
+    import torch
+    n = 320
+    for dominant, far in ((0, 8), (9, 1)):
+        c = _new(1, 1, 1, [n], 32, "int8", "bf16")
+        k = torch.zeros(1, 1, n, 128)
+        k[0, 0, 32 * dominant:32 * dominant + 32, 0] = 100.0
+        v = 2.0 ** -90 * _rows(65, 1, 1, n, 128).double()
+        v[0, 0, 32 * far:32 * far + 32] *= 2.0 ** 180
+        _append(c, 0, k.to(torch.bfloat16), v.to(torch.bfloat16), [0], [n])
+        q = torch.zeros(1, 1, n_q, 128)
+        q[..., 0] = 1.0
+        out = _attend(c, [n], q.to(torch.bfloat16), [n_q], cross=True, sm=math.log(2.0))  # scores: the first channel, in log2 units
+        kk, vv = oq.read_sequence(_numpy(c), 0, 0, 0, n, "int8")
+        ref, bound = oq.attention(q[0, 0].double().numpy(), kk, vv * 2.0 ** 10, np.full(n_q, n), math.log(2.0), HALF["bf16"])
+        r = np.abs(out[0, 0].double().cpu().numpy() * 2.0 ** 10 - ref) / bound
+        _say(f"small weights rows {n_q} dominant block {dominant}: largest {np.abs(ref).max():.3f}, worst err / bound {r.max():.3f}")
+        assert r.max() <= 1
+
+
+@pytest.mark.parametrize("case", ["dominant", "zero blocks"])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_uneven_values_many_rows(fmt, case):
+    """The prompts' kernel on tokens that dominate and on blocks of zero values that take most of the attention."""
+    import torch
+    n, n_q = 1500, 200
+    c = _new(1, 1, 2, [n], 64, fmt)
+    g = torch.Generator().manual_seed(67)
+    k, v = 0.1 * torch.randn(1, 1, n, 128, generator=g), 1e-2 * torch.randn(1, 1, n, 128, generator=g)
+    if case == "dominant":
+        at = torch.arange(5, n, 200)
+        k[0, 0, at, 0] = torch.linspace(10, 30, len(at))
+        v[0, 0] *= torch.where(torch.arange(n) % 200 < 32, 2.0 ** -9, 8.0)[:, None]
+    else:
+        k[0, 0, 32:64, 0] += 8.0
+        v[0, 0, 32:64] = 0.0
+        v[0, 0, 320:352] = -0.0
+    _append(c, 0, k.half(), v.half(), [0], [n])
+    q = torch.zeros(1, 2, n_q, 128)
+    q[:, 0, :, 0] = math.log(2.0) / SM  # scores of head 0 are the first channel, in log2 units; head 1 sees all alike
+    q = q.half()
+    out = _attend(c, [n], q, [n_q])
+    _check_attention(c, out, [n], q, [n_q], fmt, "fp16", f"uneven {fmt} {case}", rows=np.array([0, 50, n_q - 1]))
