@@ -475,7 +475,8 @@ typedef struct {               /* rows of 128 channels: element (b, h, t, c) at 
 /* Rotate queries and keys, from any row layout into any other (projections leave them token by token,
  * the caches take them head by head), in one launch.
  *   params     host
- *   q, k       device rows [batch][q_heads or kv_heads][n_tokens], or NULL for none of the kind
+ *   q, k       device rows [batch][q_heads or kv_heads][n_tokens], or NULL for none of the kind (with n_tokens
+ *              0 the addresses of rows and positions may be NULL too)
  *   positions  device i32 [batch][3][n_tokens], any values
  *   lens_host  host i32 [batch], 0 <= lens_host[b] <= n_tokens: rows t < lens_host[b] are rotated, the
  *              others are neither read nor written; NULL: all of them
@@ -560,7 +561,7 @@ size_t okvq_q8_buffer_bytes(const okvq_q8_dims* dims, int32_t which_buffer);
  * the lengths: row i of sequence b is token seq_lens[b] - n_new[b] + i.
  *   layer       0 .. L - 1
  *   lens_host   host i32 [B], the lengths with the new tokens, 0 <= lens_host[b] <= max_pages * T
- *   k_new, v_new  device [B][H][n_max][128]; rows i >= n_new[b] are not read
+ *   k_new, v_new  device [B][H][n_max][128], finite (may be NULL with n_max 0); rows i >= n_new[b] are not read
  *   n_new_host  host i32 [B], n_new_dev the same on the device, 0 <= n_new <= n_max, n_new <= lens */
 okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* k_new,
                            const uint16_t* v_new, const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max,
@@ -574,20 +575,24 @@ size_t okvq_q8_workspace_bytes(const okvq_q8_dims* dims, int32_t max_seq_len, in
 /* Attention of new rows over one layer of the 8-bit cache: one token a sequence (a decode step: the
  * sequence is split over the GPU), a chunk, or a whole prompt.
  *   lens_host   host i32 [B]: lengths with the new tokens (plans the launch; the kernels read seq_lens)
- *   q           device [B][Hq][n_max][128]; query head j reads KV head j / G
+ *   q           device [B][Hq][n_max][128], finite; query head j reads KV head j / G. q and out may be NULL with
+ *               n_max 0
  *   n_new_host, n_new_dev  rows of each sequence, 0 <= n_new <= n_max
- *   sm_scale    softmax scale, finite
+ *   sm_scale    softmax scale, finite also times log2(e)
  *   out         device [B][Hq][n_max][128] of the rows' type; rows i >= n_new[b] are left as they were
  *   workspace   device, 16-byte aligned, okvq_q8_workspace_bytes(dims, max(lens_host), n_max) bytes
  *   flags       0: row i sees tokens 0 .. seq_lens[b] - n_new[b] + i (causal). OKVQ_Q8_CROSS: every row
  *               sees all seq_lens[b] tokens (cross attention to a cache of an encoder's states)
  * A row that sees no token yields zeros. Codes enter the matrix cores exactly as fp16, softmax statistics
- * and sums are fp32; the softmax weights times a block's value scale are rounded to fp16. */
+ * and sums are fp32; the softmax weights times a block's value scale are rounded to fp16. Scores have to stay
+ * inside +-1e30; a weight below 2^-112 of its row's largest may count as nothing, and so do values of a block
+ * whose scale is below 2^-126. */
 okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
                               const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, float sm_scale,
                               uint16_t* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
 
-/* Device workspace bytes of okvq_q8_extend and okvq_q8_compact (0 for invalid dims). No initial contents. */
+/* Device workspace bytes of okvq_q8_extend and okvq_q8_compact (0 for invalid dims). No initial contents; calls that
+ * may overlap (on different caches) need one each. */
 size_t okvq_q8_page_workspace_bytes(const okvq_q8_dims* dims);
 
 /* Make room for n_new[b] tokens in every slot and advance seq_lens by them. Pages are taken in the order

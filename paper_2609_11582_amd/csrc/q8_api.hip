@@ -85,8 +85,11 @@ okvq_status check_rows(const okvq_q8_dims& d, const int32_t* lens, const int32_t
   return OKVQ_OK;
 }
 
-okvq_status check_rows_of(const okvq_rows* r) {
-  if (!aligned16(r->data)) return OKVQ_ERR_INVALID_ARGUMENT;
+// rows' address of a call with n_max rows: an empty array may be NULL
+bool rows_at(const void* p, int32_t n_max) { return aligned16(p) || (p == nullptr && n_max == 0); }
+
+okvq_status check_rows_of(const okvq_rows* r, int32_t n_tokens) {
+  if (!rows_at(r->data, n_tokens)) return OKVQ_ERR_INVALID_ARGUMENT;
   for (int64_t s : {r->batch_stride, r->head_stride, r->token_stride})
     if (s < 0 || s % 8 != 0) return OKVQ_ERR_INVALID_ARGUMENT;
   return OKVQ_OK;
@@ -114,7 +117,7 @@ extern "C" {
 okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t n_tokens,
                         const okvq_rows* q, const okvq_rows* k, const int32_t* positions, const int32_t* lens_host,
                         const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype, uint32_t flags, void* stream) {
-  if (!params || batch < 1 || batch > 65535 || n_tokens < 0 || !aligned16(positions)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!params || batch < 1 || batch > 65535 || n_tokens < 0 || !rows_at(positions, n_tokens)) return OKVQ_ERR_INVALID_ARGUMENT;
   if (flags & ~(uint32_t)(OKVQ_ROTARY_INVERSE | OKVQ_ROTARY_ADJACENT)) return OKVQ_ERR_INVALID_ARGUMENT;
   if (dtype != OKVQ_F16 && dtype != OKVQ_BF16) return OKVQ_ERR_INVALID_ARGUMENT;
   if (!q != !q_out || !k != !k_out || (!q && !k)) return OKVQ_ERR_INVALID_ARGUMENT;
@@ -122,7 +125,7 @@ okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t
   const int hq = q ? q_heads : 0, hk = k ? kv_heads : 0;
   if ((int64_t)hq + hk > 65535) return OKVQ_ERR_UNSUPPORTED;
   for (const okvq_rows* r : {q, k, q_out, k_out})
-    if (r && check_rows_of(r) != OKVQ_OK) return OKVQ_ERR_INVALID_ARGUMENT;
+    if (r && check_rows_of(r, n_tokens) != OKVQ_OK) return OKVQ_ERR_INVALID_ARGUMENT;
   RotaryArgs a;
   a.q = a.k = a.q_out = a.k_out = okvq_rows{};
   for (int i = 0; i < 64; ++i) {
@@ -189,7 +192,7 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
   if (st != OKVQ_OK) return st;
   const okvq_q8_dims& d = cache->dims;
   if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0) return OKVQ_ERR_INVALID_ARGUMENT;
-  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(n_new_dev)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!rows_at(k_new, n_max) || !rows_at(v_new, n_max) || !aligned16(n_new_dev)) return OKVQ_ERR_INVALID_ARGUMENT;
   int max_len, most;
   st = check_rows(d, lens_host, n_new_host, n_max, false, &max_len, &most);
   if (st != OKVQ_OK) return st;
@@ -212,10 +215,11 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
   okvq_status st = check_cache(cache);
   if (st != OKVQ_OK) return st;
   const okvq_q8_dims& d = cache->dims;
-  if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0 || !std::isfinite(sm_scale) ||
+  const float qscale = sm_scale * 1.4426950408889634f;  // log2(e): the kernels' exponentials have base 2
+  if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0 || !std::isfinite(qscale) ||
       (flags & ~(uint32_t)OKVQ_Q8_CROSS))
     return OKVQ_ERR_INVALID_ARGUMENT;
-  if (!aligned16(q) || !aligned16(n_new_dev) || !aligned16(out)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!rows_at(q, n_max) || !aligned16(n_new_dev) || !rows_at(out, n_max)) return OKVQ_ERR_INVALID_ARGUMENT;
   int max_len, most;
   st = check_rows(d, lens_host, n_new_host, n_max, true, &max_len, &most);
   if (st != OKVQ_OK) return st;
@@ -237,7 +241,7 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
   a.n_max = n_max;
   a.G = G;
   a.cross = (flags & OKVQ_Q8_CROSS) ? 1 : 0;
-  a.qscale = sm_scale * 1.4426950408889634f;
+  a.qscale = qscale;
   return hip_status(launch_q8_attention(a, plan, d.format, d.dtype, d.batch, static_cast<hipStream_t>(stream)));
 }
 

@@ -758,3 +758,20 @@ def test_uneven_values_many_rows(fmt, case):
     q = q.half()
     out = _attend(c, [n], q, [n_q])
     _check_attention(c, out, [n], q, [n_q], fmt, "fp16", f"uneven {fmt} {case}", rows=np.array([0, 50, n_q - 1]))
+
+
+def test_empty_rows():
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    c = _filled(2, 1, 4, [40, 3], 64, "int8", "fp16", 71)
+    before, zero = {f: t.clone() for f, t in c.buffers.items()}, _i32([0, 0])
+    none = torch.empty(2, 1, 0, 128, dtype=torch.float16, device="cuda")
+    okvq.okvq_q8_append(c, 0, [40, 3], none, none, [0, 0], zero, 0)
+    q = torch.empty(2, 4, 0, 128, dtype=torch.float16, device="cuda")
+    okvq.okvq_q8_attention(c, 0, [40, 3], q, [0, 0], zero, 0, SM, q.clone(), okvq.q8_workspace(c.dims, 40))
+    rot = okvq.make_rotary([1.0] * 64, [0] * 64)
+    okvq.okvq_rotary(rot, q, none, torch.empty(2, 3, 0, dtype=torch.int32, device="cuda"), q, none)
+    torch.cuda.synchronize()
+    for f, t in c.buffers.items():
+        assert torch.equal(t.view(torch.uint8), before[f].view(torch.uint8)), f

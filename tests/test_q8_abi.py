@@ -148,3 +148,25 @@ def test_binding_refuses_host_tensors():
         q8.okvq_rotary(par, x, None, torch.zeros(1, 3, 4, dtype=torch.int32), x, None)
     with pytest.raises(ValueError):
         q8.okvq_rotary(par, None, None, torch.zeros(1, 3, 4, dtype=torch.int32), None, None)
+
+
+def test_empty_rows_may_be_null():
+    """torch gives an empty tensor no address."""
+    L, d = q8.lib(), dims()
+    c, none = ctypes.byref(cache(d)), i32(0, 0)
+    assert L.okvq_q8_append(c, 0, i32(5, 5), None, None, none, FAKE, 0, None) == 0
+    assert L.okvq_q8_append(c, 0, i32(5, 5), None, FAKE, none, FAKE, 1, None) == -1
+    assert L.okvq_q8_attention(c, 0, i32(5, 5), None, none, FAKE, 0, ctypes.c_float(0.1), None, FAKE, 0, 0, None) == 0
+    assert L.okvq_q8_attention(c, 0, i32(5, 5), None, none, FAKE, 1, ctypes.c_float(0.1), FAKE, FAKE, 0, 0, None) == -1
+    empty = ctypes.byref(q8.Rows(None, 0, 0, 0))
+    par = ctypes.byref(q8.make_rotary([0.5] * 64, [0] * 64))
+    assert L.okvq_rotary(par, 1, 2, 2, 0, empty, empty, None, None, empty, empty, 0, 0, None) == 0
+    assert L.okvq_rotary(par, 1, 2, 2, 1, empty, empty, FAKE, None, empty, empty, 0, 0, None) == -1
+
+
+def test_softmax_scale_past_the_range_of_base_two():
+    d = dims()
+    for sm, want in ((3.0e38, -1), (-3.0e38, -1), (2.0e38, 0)):
+        st = q8.lib().okvq_q8_attention(ctypes.byref(cache(d)), 0, i32(5, 5), FAKE, i32(0, 0), FAKE, 1, ctypes.c_float(sm), FAKE, FAKE, 0, 0,
+                                        None)
+        assert st == want
