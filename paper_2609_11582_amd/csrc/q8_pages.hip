@@ -106,7 +106,14 @@ __device__ __forceinline__ void copy_pages(const Q8Pages& c, const int32_t* pair
   }
 }
 
-__global__ __launch_bounds__(kCopyThreads) void k_q8_copy(Q8Pages c, Q8PageWs ws) {
+// Copies of the plan; of a compaction (places) also every table entry becomes its page's new place, ws.list
+__global__ __launch_bounds__(kCopyThreads) void k_q8_copy(Q8Pages c, Q8PageWs ws, bool places) {
+  if (places)
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < (int64_t)c.B * c.max_pages;
+         i += (int64_t)gridDim.x * kCopyThreads) {
+      const int id = c.table[i];
+      if (id >= 0 && id < c.P) c.table[i] = ws.list[id];
+    }
   copy_pages(c, ws.pairs, ws.count[0], blockIdx.x, gridDim.x, threadIdx.x);
 }
 
@@ -264,17 +271,11 @@ __global__ __launch_bounds__(kPlan) void k_q8_compact(Q8Pages c, Q8PageWs ws) {
   }
 }
 
-__global__ __launch_bounds__(256) void k_q8_remap(Q8Pages c, Q8PageWs ws) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)c.B * c.max_pages; i += (int64_t)gridDim.x * 256) {
-    const int id = c.table[i];
-    if (id >= 0 && id < c.P) c.table[i] = ws.list[id];
-  }
-}
-
-hipError_t launch_copy(const Q8Pages& c, const Q8PageWs& w, int most, hipStream_t s) {
+hipError_t launch_copy(const Q8Pages& c, const Q8PageWs& w, int most, bool places, hipStream_t s) {
   const int64_t page_bytes = (int64_t)c.H * c.T * kD;
-  const int64_t units = (int64_t)most * c.L * 2 * ((page_bytes + kCopyBytes - 1) / kCopyBytes);
-  hipLaunchKernelGGL(k_q8_copy, dim3((unsigned)std::min<int64_t>(units, 2048)), dim3(kCopyThreads), 0, s, c, w);
+  int64_t units = (int64_t)most * c.L * 2 * ((page_bytes + kCopyBytes - 1) / kCopyBytes);
+  if (places) units = std::max(units, ((int64_t)c.B * c.max_pages + kCopyThreads - 1) / kCopyThreads);
+  hipLaunchKernelGGL(k_q8_copy, dim3((unsigned)std::min<int64_t>(units, 2048)), dim3(kCopyThreads), 0, s, c, w, places);
   return hipGetLastError();
 }
 
@@ -302,7 +303,7 @@ hipError_t launch_q8_extend(const Q8Pages& c, const int32_t* n_new, int32_t* gra
   hipLaunchKernelGGL(k_q8_extend, dim3(1), dim3(kPlan), 0, s, c, n_new, granted, w, copy_here);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || copy_here) return e;
-  return launch_copy(c, w, c.B, s);
+  return launch_copy(c, w, c.B, false, s);
 }
 
 hipError_t launch_q8_fork(const Q8Pages& c, const LenArgs& src, const LenArgs& dst, int n, hipStream_t s) {
@@ -320,11 +321,7 @@ hipError_t launch_q8_compact(const Q8Pages& c, void* ws, hipStream_t s) {
   hipLaunchKernelGGL(k_q8_compact, dim3(1), dim3(kPlan), 0, s, c, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t entries = (int64_t)c.B * c.max_pages;
-  hipLaunchKernelGGL(k_q8_remap, dim3((unsigned)std::min<int64_t>((entries + 255) / 256, 2048)), dim3(256), 0, s, c, w);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  return launch_copy(c, w, c.P / 2 + 1, s);
+  return launch_copy(c, w, c.P / 2 + 1, true, s);
 }
 
 }  // namespace okvq
