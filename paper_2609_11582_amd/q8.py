@@ -5,12 +5,13 @@ type; the stream is torch's current one unless one is given."""
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 from typing import Sequence
 
 import torch
 
-from .okvq import OkvqError, _check, _i32, _need_len, _stream
+from .okvq import OkvqError, _check, _need_len, _stream
 from .okvq import lib as _okvq_lib
 
 OKVQ_F16 = 0
@@ -55,16 +56,16 @@ def lib() -> ctypes.CDLL:
         L = _okvq_lib()
         vp, i32, u32, sz, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t, ctypes.POINTER
         for name, res, args in (
-                # okvq_rows as packed bytes (_rows_of) or Rows structures
-                ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, P(i32), vp, vp, i32, u32, vp]),
+                # okvq_rows as packed bytes (_rows_of) or Rows structures, host counts as packed bytes (_ints) or arrays
+                ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, u32, vp]),
                 ("okvq_q8_buffer_bytes", sz, [P(Q8Dims), i32]),
-                ("okvq_q8_append", i32, [P(Q8Struct), i32, P(i32), vp, vp, P(i32), vp, i32, vp]),
+                ("okvq_q8_append", i32, [P(Q8Struct), i32, vp, vp, vp, vp, vp, i32, vp]),
                 ("okvq_q8_workspace_bytes", sz, [P(Q8Dims), i32, i32]),
-                ("okvq_q8_attention", i32, [P(Q8Struct), i32, P(i32), vp, P(i32), vp, i32, ctypes.c_float, vp, vp, sz, u32, vp]),
+                ("okvq_q8_attention", i32, [P(Q8Struct), i32, vp, vp, vp, vp, i32, ctypes.c_float, vp, vp, sz, u32, vp]),
                 ("okvq_q8_page_workspace_bytes", sz, [P(Q8Dims)]),
                 ("okvq_q8_extend", i32, [P(Q8Struct), vp, vp, vp, sz, vp]),
-                ("okvq_q8_fork", i32, [P(Q8Struct), P(i32), P(i32), i32, vp]),
-                ("okvq_q8_free", i32, [P(Q8Struct), P(i32), i32, vp]),
+                ("okvq_q8_fork", i32, [P(Q8Struct), vp, vp, i32, vp]),
+                ("okvq_q8_free", i32, [P(Q8Struct), vp, i32, vp]),
                 ("okvq_q8_compact", i32, [P(Q8Struct), vp, sz, vp]),
                 ("okvq_q8_status", i32, [P(Q8Struct), P(i32), vp])):
             f = getattr(L, name)
@@ -95,13 +96,30 @@ def _refuse(t, name: str, device: int):
     raise ValueError(f"{name}: on {t.device}, but the current device is {device}")
 
 
-def _ints(xs: Sequence[int], n: int, name: str):
+def _int(x, name: str, low=-(1 << 31), high=(1 << 31) - 1) -> int:
+    """x as a whole number of 32 bits: ctypes would drop the bits above them."""
+    x = int(x)
+    if not low <= x <= high:
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return x
+
+
+@functools.lru_cache(maxsize=None)
+def _int_packer(n: int):
+    return struct.Struct(f"{n}i").pack
+
+
+def _ints(xs: Sequence[int], n: int, name: str) -> bytes:
+    """int32 [n] as packed bytes, which refuse what 32 bits do not hold."""
     if len(xs) != n:
         raise ValueError(f"{name}: {len(xs)} entries, expected {n}")
     try:
-        return (ctypes.c_int32 * n)(*xs)
-    except TypeError:  # numpy integers and the like
-        return _i32(xs)
+        return _int_packer(n)(*xs)
+    except struct.error:
+        try:
+            return _int_packer(n)(*[int(x) for x in xs])
+        except struct.error:
+            raise ValueError(f"{name}: entries have to fit 32 bits") from None
 
 
 # ---- rotary positions ----------------------------------------------------------------------------
@@ -158,7 +176,7 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
     if positions.shape != (B, 3, n):
         raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
     st = lib().okvq_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, pos, None if lens is None else _ints(lens, B, "lens"),
-                           oq, ok, _ROW_TYPES[dt], int(flags), _stream(stream))
+                           oq, ok, _ROW_TYPES[dt], _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_rotary")
     return st
@@ -169,12 +187,14 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
 
 def make_q8_dims(batch, num_kv_heads, num_q_heads, num_pages, max_pages, layers=1, page_tokens=64, format="int8",  # noqa: A002
                  dtype="fp16", head_dim=128) -> Q8Dims:
-    return Q8Dims(layers, batch, num_kv_heads, num_q_heads, head_dim, num_pages, page_tokens, max_pages, Q8_FORMATS[format],
-                  Q8_DTYPES[dtype][0])
+    sizes = layers, batch, num_kv_heads, num_q_heads, head_dim, num_pages, page_tokens, max_pages
+    for x, (name, _) in zip(sizes, Q8Dims._fields_):
+        _int(x, name)
+    return Q8Dims(*sizes, Q8_FORMATS[format], Q8_DTYPES[dtype][0])
 
 
 def okvq_q8_buffer_bytes(dims: Q8Dims, which: int) -> int:
-    return lib().okvq_q8_buffer_bytes(ctypes.byref(dims), which)
+    return lib().okvq_q8_buffer_bytes(ctypes.byref(dims), _int(which, "which"))
 
 
 class Q8Cache:
@@ -223,9 +243,9 @@ def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, 
     """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128]) into one layer's pages, after
     okvq_q8_extend; lens: the lengths with them."""
     B, H, _ = cache._sizes
-    dev, dt, n_max = _device(), cache.row_dtype, int(n_max)
+    dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
     nbytes = B * H * n_max * 256
-    st = lib().okvq_q8_append(_cache_ref(cache, dev), int(layer), _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
+    st = lib().okvq_q8_append(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
                               _need(v_new, nbytes, dt, "v_new", dev), _ints(n_new, B, "n_new"),
                               _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, _stream(stream))
     if check and st:
@@ -234,7 +254,7 @@ def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, 
 
 
 def okvq_q8_workspace_bytes(dims: Q8Dims, max_seq_len: int, n_max: int = 1) -> int:
-    return lib().okvq_q8_workspace_bytes(ctypes.byref(dims), int(max_seq_len), int(n_max))
+    return lib().okvq_q8_workspace_bytes(ctypes.byref(dims), _int(max_seq_len, "max_seq_len"), _int(n_max, "n_max"))
 
 
 def q8_workspace(dims: Q8Dims, max_seq_len: int, n_max: int = 1, device="cuda") -> torch.Tensor:
@@ -248,12 +268,12 @@ def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, s
     """Attention of rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
     tokens of each sequence, causal, or OKVQ_Q8_CROSS. lens: the lengths with the new tokens."""
     B, _, Hq = cache._sizes
-    dev, dt, n_max = _device(), cache.row_dtype, int(n_max)
+    dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
     nbytes = B * Hq * n_max * 256
-    st = lib().okvq_q8_attention(_cache_ref(cache, dev), int(layer), _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
+    st = lib().okvq_q8_attention(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
                                  _ints(n_new, B, "n_new"), _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, float(sm_scale),
                                  _need(out, nbytes, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
-                                 int(flags), _stream(stream))
+                                 _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_q8_attention")
     return st
