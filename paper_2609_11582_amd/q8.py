@@ -90,6 +90,14 @@ def _need(t: torch.Tensor, nbytes: int, dtype, name: str, device: int) -> int:
     return t.data_ptr()
 
 
+def _need_rows(t: torch.Tensor, shape, dtype, name: str, device: int) -> int:
+    """The address of contiguous rows of this shape, dimensions of one entry aside: as many bytes in another order (token by
+    token, or rows of a longer buffer) would be read as other rows."""
+    if isinstance(t, torch.Tensor) and t.shape != shape and [n for n in t.shape if n != 1] != [n for n in shape if n != 1]:
+        raise ValueError(f"{name}: {list(t.shape)}, expected {list(shape)}")
+    return _need(t, 0, dtype, name, device)
+
+
 def _refuse(t, name: str, device: int):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous device tensor")
@@ -240,13 +248,13 @@ def _cache_ref(cache: Q8Cache, device: int):
 
 
 def okvq_q8_append(cache: Q8Cache, layer, lens, k_new, v_new, n_new, n_new_dev, n_max, stream=None, check=True) -> int:
-    """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128]) into one layer's pages, after
-    okvq_q8_extend; lens: the lengths with them."""
+    """Quantize the newest n_new[b] tokens (rows of k_new, v_new [B][H][n_max][128], contiguous) into one layer's pages,
+    after okvq_q8_extend; lens: the lengths with them."""
     B, H, _ = cache._sizes
     dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
-    nbytes = B * H * n_max * 256
-    st = lib().okvq_q8_append(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need(k_new, nbytes, dt, "k_new", dev),
-                              _need(v_new, nbytes, dt, "v_new", dev), _ints(n_new, B, "n_new"),
+    shape = (B, H, n_max, 128)
+    st = lib().okvq_q8_append(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need_rows(k_new, shape, dt, "k_new", dev),
+                              _need_rows(v_new, shape, dt, "v_new", dev), _ints(n_new, B, "n_new"),
                               _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, _stream(stream))
     if check and st:
         _check(st, "okvq_q8_append")
@@ -265,14 +273,14 @@ def q8_workspace(dims: Q8Dims, max_seq_len: int, n_max: int = 1, device="cuda") 
 
 def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, sm_scale, out, workspace, flags=0,
                       stream=None, check=True) -> int:
-    """Attention of rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
+    """Attention of contiguous rows q [B][Hq][n_max][128] over one layer into out (same shape and type): the newest n_new[b]
     tokens of each sequence, causal, or OKVQ_Q8_CROSS. lens: the lengths with the new tokens."""
     B, _, Hq = cache._sizes
     dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
-    nbytes = B * Hq * n_max * 256
-    st = lib().okvq_q8_attention(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need(q, nbytes, dt, "q", dev),
+    shape = (B, Hq, n_max, 128)
+    st = lib().okvq_q8_attention(_cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need_rows(q, shape, dt, "q", dev),
                                  _ints(n_new, B, "n_new"), _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, float(sm_scale),
-                                 _need(out, nbytes, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
+                                 _need_rows(out, shape, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes,
                                  _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_q8_attention")

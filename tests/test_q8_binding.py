@@ -54,3 +54,30 @@ def test_other_arguments_past_32_bits(cache):
         sizes[name] = WRAP + sizes.get(name, 64)
         with pytest.raises(ValueError):
             q8.make_q8_dims(**sizes)
+
+
+@pytest.mark.parametrize("shape", [(2, 5, 2, 128), (2, 2, 6, 128), (4, 5, 128), (2, 2, 5, 256), (3, 2, 5, 128)])
+def test_rows_in_another_order(cache, shape):
+    """Enough bytes are not enough: rows that lie token by token, a longer buffer's rows."""
+    good, bad = (torch.zeros(s, dtype=torch.float16) for s in ((2, 2, 5, 128), shape))
+    n_dev, none, ws = torch.zeros(4, dtype=torch.int32), (0, 0), q8.q8_workspace(cache.dims, 64, 5, device="cpu")
+
+    def append(k, v):
+        return q8.okvq_q8_append(cache, 0, (9, 9), k, v, none, n_dev, 5, stream=0)
+
+    def attend(q, out):
+        return q8.okvq_q8_attention(own_heads, 0, (9, 9), q, none, n_dev, 5, 0.1, out, ws, stream=0)
+    own_heads = q8.Q8Cache(2, 2, 2, 10, 4, device="cpu")
+    for call in (append, attend):
+        assert call(good, good) == 0
+        for pair in ((bad, good), (good, bad)):
+            with pytest.raises(ValueError):
+                call(*pair)
+
+
+@pytest.mark.parametrize("shape", [(2, 2, 128), (2, 1, 2, 128), (2, 2, 1, 128)])
+def test_dimensions_of_one_entry_move_nothing(cache, shape):
+    x = torch.zeros(shape, dtype=torch.float16)
+    assert q8.okvq_q8_append(cache, 0, (9, 9), x, x, (0, 0), torch.zeros(4, dtype=torch.int32), 1, stream=0) == 0
+    with pytest.raises(ValueError):
+        q8.okvq_q8_append(cache, 0, (9, 9), x, x, (0, 0), torch.zeros(4, dtype=torch.int32), 2, stream=0)
