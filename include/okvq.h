@@ -481,7 +481,8 @@ typedef struct {               /* rows of 128 channels: element (b, h, t, c) at 
  *   lens_host  host i32 [batch], 0 <= lens_host[b] <= n_tokens: rows t < lens_host[b] are rotated, the
  *              others are neither read nor written; NULL: all of them
  *   q_out, k_out  device rows; an output may be its own input with the same strides (in place) and
- *              may not overlap an input otherwise
+ *              may not overlap an input otherwise. Its rows may not overlap each other (an input's may): by growing
+ *              stride, a dimension of more than one entry has to step over all rows of those before it
  *   dtype      OKVQ_F16 or OKVQ_BF16, of inputs and outputs
  *   flags      OKVQ_ROTARY_INVERSE, OKVQ_ROTARY_ADJACENT
  * The angle is formed as a 64-bit fraction of a turn, so that far positions lose nothing; the rotation

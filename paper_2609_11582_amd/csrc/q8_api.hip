@@ -2,6 +2,7 @@
 // Declarations and contracts: include/okvq.h.
 #include <algorithm>
 #include <cmath>
+#include <utility>
 
 #include "q8.hpp"
 
@@ -95,6 +96,18 @@ okvq_status check_rows_of(const okvq_rows* r, int32_t n_tokens) {
   return OKVQ_OK;
 }
 
+// Rows that are written may not overlap: by growing stride, a dimension steps over all rows of those before it
+bool rows_apart(const okvq_rows& r, int64_t batch, int64_t heads, int64_t tokens) {
+  std::pair<int64_t, int64_t> dim[3] = {{r.batch_stride, batch}, {r.head_stride, heads}, {r.token_stride, tokens}};
+  std::sort(dim, dim + 3);
+  __int128 span = kD;
+  for (const auto& [stride, n] : dim) {
+    if (n > 1 && stride < span) return false;
+    if (n > 1) span += (__int128)stride * (n - 1);
+  }
+  return true;
+}
+
 // distinct slots of B; `seen` marks them (arrays on the stack: nothing here throws)
 okvq_status check_slots(const int32_t* slots, int n, int B, bool (&seen)[kQ8MaxBatch]) {
   for (int i = 0; i < n; ++i) {
@@ -150,9 +163,14 @@ okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t
   a.hk = hk;
   a.n = n_tokens;
   a.flags = flags;
+  int longest = lens_host ? 0 : n_tokens;
   if (lens_host)
-    for (int b = 0; b < batch; ++b)
+    for (int b = 0; b < batch; ++b) {
       if (lens_host[b] < 0 || lens_host[b] > n_tokens) return OKVQ_ERR_INVALID_ARGUMENT;
+      longest = std::max(longest, lens_host[b]);
+    }
+  if (longest > 0 && ((q && !rows_apart(*q_out, batch, hq, longest)) || (k && !rows_apart(*k_out, batch, hk, longest))))
+    return OKVQ_ERR_INVALID_ARGUMENT;
   for (int b0 = 0; b0 < batch; b0 += kMaxLenArgs) {
     a.b0 = b0;
     a.nb = std::min(kMaxLenArgs, batch - b0);

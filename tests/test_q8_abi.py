@@ -170,3 +170,19 @@ def test_softmax_scale_past_the_range_of_base_two():
         st = q8.lib().okvq_q8_attention(ctypes.byref(cache(d)), 0, i32(5, 5), FAKE, i32(0, 0), FAKE, 1, ctypes.c_float(sm), FAKE, FAKE, 0, 0,
                                         None)
         assert st == want
+
+
+def test_rotary_outputs_whose_rows_overlap():
+    """Rows that would overwrite each other in any order: a dimension without a stride, or one within another's rows. Rows that
+    lens leaves out do not count."""
+    L = q8.lib()
+    par = ctypes.byref(q8.make_rotary([0.5] * 64, [0] * 64))
+    ok = ctypes.byref(q8.Rows(4096, 128 * 8, 128 * 4, 128))
+    for batch, heads, n, bad in ((1, 2, 4, (0, 0, 128)), (1, 2, 4, (0, 512, 0)), (2, 2, 4, (0, 512, 128)), (1, 2, 4, (0, 384, 128)),
+                                 (1, 2, 4, (0, 128, 128)), (1, 1, 4, (0, 0, 120)), (2, 2, 4, (960, 512, 128)), (2, 1, 2, (8, 0, 256))):
+        out = ctypes.byref(q8.Rows(8192, *bad))
+        for where in (dict(qo=out), dict(ko=out)):
+            args = {"qo": ok, "ko": ok, **where}
+            st = L.okvq_rotary(par, batch, heads, heads, n, ok, ok, FAKE, None, args["qo"], args["ko"], 0, 0, None)
+            assert st == -1, (batch, heads, n, bad)
+        assert L.okvq_rotary(par, batch, heads, heads, n, ok, ok, FAKE, i32(*[0] * batch), out, out, 0, 0, None) == 0
