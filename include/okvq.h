@@ -485,8 +485,9 @@ typedef struct {               /* rows of 128 channels: element (b, h, t, c) at 
  *              stride, a dimension of more than one entry has to step over all rows of those before it
  *   dtype      OKVQ_F16 or OKVQ_BF16, of inputs and outputs
  *   flags      OKVQ_ROTARY_INVERSE, OKVQ_ROTARY_ADJACENT
- * The angle is formed as a 64-bit fraction of a turn, so that far positions lose nothing; the rotation
- * is computed in fp32 and rounded once. 1 <= batch <= 65535, heads up to 65535 together. */
+ * The angle is formed as a 64-bit fraction of a turn, so that far positions lose nothing (at frequencies up to some
+ * turns a position: the fraction is off by position * max(|inv_freq| / 2 pi, 1) * 2^-63 of a turn at most); the
+ * rotation is computed in fp32 and rounded once. 1 <= batch <= 65535, heads up to 65535 together. */
 okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
                         int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const int32_t* positions,
                         const int32_t* lens_host, const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype,

@@ -144,11 +144,12 @@ okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t
   for (int i = 0; i < 64; ++i) {
     if (params->axis[i] > 2 || !std::isfinite(params->inv_freq[i])) return OKVQ_ERR_INVALID_ARGUMENT;
     a.axis[i] = params->axis[i];
-    // turns per position, modulo one (positions are whole numbers), in units of 2^-64
-    double t = params->inv_freq[i] / (2.0 * M_PI);
+    // Turns per position, modulo one (positions are whole numbers), in units of 2^-64. In extended precision: a double's
+    // quotient is 2^-53 off, 2^-22 of the frequency at position 2^31
+    long double t = params->inv_freq[i] / 6.283185307179586476925286766559L;
     t -= std::floor(t);
-    const double scaled = t * 0x1p64;
-    a.turn[i] = scaled < 0x1p64 ? (uint64_t)scaled : 0;
+    const long double scaled = t * 0x1p64L;
+    a.turn[i] = scaled < 0x1p64L ? (uint64_t)scaled : 0;
   }
   if (q) {
     a.q = *q;

@@ -182,3 +182,32 @@ def test_refuses_wrong_tensors():
     odd = torch.zeros(1, 2, 4, 132, dtype=torch.float16, device="cuda")[..., :128]  # rows 264 bytes apart
     with pytest.raises(okvq.OkvqError):
         okvq.okvq_rotary(par, odd, None, pos, x, None)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_far_positions_of_high_frequencies(sign):
+    """Frequencies of half a turn to a whole one per position, at positions around 2^31: within the tolerance of near ones, as
+    the fraction of a turn is exact to 2^31 * 2^-63 of a turn."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    g = torch.Generator().manual_seed(9)
+    freq = [sign * float(f) for f in 3.2 + 3.0 * torch.rand(64, generator=g, dtype=torch.float64)]
+    x = torch.randn(2, 300, 4, 128, generator=g).half()
+    pos = torch.randint((1 << 31) - 100000, (1 << 31) - 1, (2, 3, 300), generator=g)
+    pos[1] = -1 - pos[1]
+    pos = pos.to(torch.int32)
+    d = x.cuda().transpose(1, 2)
+    out = torch.empty_like(d)
+    okvq.okvq_rotary(okvq.make_rotary(freq, AXES), None, d, pos.cuda(), None, out)
+    turn = 2 * np.longdouble(np.pi) + np.longdouble(2 * 1.2246467991473532e-16)  # pi and what a double leaves of it
+    turns = pos.numpy()[:, AXES, :].astype(np.longdouble).transpose(0, 2, 1)[:, None] * (np.array(freq, np.longdouble) / turn)
+    angle = ((turns - np.rint(turns)) * turn).astype(np.float64)
+    xs = x.transpose(1, 2).double().numpy()
+    c, s = np.cos(angle), np.sin(angle)
+    ref = np.concatenate([xs[..., :64] * c - xs[..., 64:] * s, xs[..., 64:] * c + xs[..., :64] * s], -1)
+    size = np.abs(xs[..., :64]) + np.abs(xs[..., 64:])
+    size = np.concatenate([size, size], -1)
+    err = np.abs(out.double().cpu().numpy() - ref) / (HALF["fp16"] * np.abs(ref) + 2.0 ** -21 * size + 2.0 ** -25)
+    print(f"[gpu-case] far positions of high frequencies: worst err / tolerance {err.max():.3f}", flush=True)
+    assert err.max() <= 1
