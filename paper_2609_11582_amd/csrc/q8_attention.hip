@@ -205,9 +205,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
     o += *reinterpret_cast<const floatx4*>(&cmb[w][cc * kCombineRow + ch]) * __builtin_amdgcn_exp2f(wM[w][cc] - Mt);
   }
   if (records == 0) {
-    const float f = lt > 0.0f ? __builtin_amdgcn_exp2f(Mt - mt - kWeightExp) / lt : 0.0f;
+    const RowFactor f(Mt, mt, lt);
     *reinterpret_cast<uint2*>(p.out + (((int64_t)b * c.Hq + chq) * p.n_max + ci) * kD + ch) =
-        make_uint2(row_pack<kBf16>(o[0] * f, o[1] * f), row_pack<kBf16>(o[2] * f, o[3] * f));
+        make_uint2(row_pack<kBf16>(f(o[0]), f(o[1])), row_pack<kBf16>(f(o[2]), f(o[3])));
     return;
   }
   float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit + split) * kRecFloatsQ8;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
   const int recf = cols * (kD + 4);
   const float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit) * recf;
   floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  float scale = 0.0f;
+  RowFactor factor(kNoScore, kNoScore, 0.0f);
   if (live) {
     // A group has 8 splits at most: their sums are on their way while the references and the softmax sum of all splits
     // are formed, which every group does for itself (a lane takes every 32nd split)
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 #pragma unroll
     for (int k = 0; k < kStats; ++k) l += st[k][2] * __builtin_amdgcn_exp2f(st[k][1] - m);
     l = half_reduce(l, [](float a, float b) { return a + b; });
-    scale = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
+    factor = RowFactor(M, m, l);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
       if (grp + k * kGroups < nsplit) o += v[k] * __builtin_amdgcn_exp2f(vM[k] - M);
@@ -284,9 +284,8 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
     for (int k = 1; k < kGroups; ++k) o += part[(tid >> 5) + k][lane];
   }
   if (!live) return;
-  o *= scale;
   *reinterpret_cast<uint2*>(p.out + (((int64_t)b * p.c.Hq + hq) * p.n_max + i) * kD + 4 * lane) =
-      make_uint2(row_pack<kBf16>(o[0], o[1]), row_pack<kBf16>(o[2], o[3]));
+      make_uint2(row_pack<kBf16>(factor(o[0]), factor(o[1])), row_pack<kBf16>(factor(o[2]), factor(o[3])));
 }
 
 }  // namespace

@@ -46,6 +46,20 @@ __device__ __forceinline__ half8 widen8(uint32_t a, uint32_t b) {
                                               widen2<kFmt, true>(b)));
 }
 
+// The factor 2^(M - m - kWeightExp) / l of a row's sums of products, 0 for a row without weight. The power of two may lie far
+// below fp32's normal numbers (value scales down to 2^-126, l up to 2^27 tokens), where the exponential gives zero:
+// its whole part is added to the product's exponent at the end.
+struct RowFactor {
+  float f;
+  int e;
+  __device__ __forceinline__ RowFactor(float M, float m, float l) {
+    const float x = fmaxf(M - m - kWeightExp, -1000.0f), whole = rintf(x);
+    f = l > 0.0f ? __builtin_amdgcn_exp2f(x - whole) / l : 0.0f;
+    e = (int)whole;
+  }
+  __device__ __forceinline__ float operator()(float v) const { return ldexpf(v * f, e); }
+};
+
 // A lane's query channels as fp16 operands; returns the factor that belongs to the scores. fp16 rows enter as they
 // are. bfloat16 rows are scaled by a power of two that puts the row's largest magnitude into [2^14, 2^15): their
 // 8 bits fit fp16, and what lies 2^-29 or more below the largest is lost at most. row_max: the maximum over the lanes

@@ -291,14 +291,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   l = sum32(l);
   if (!live) return;
   if (records == 0) {
-    const float f = l > 0.0f ? __builtin_amdgcn_exp2f(M - m - kWeightExp) / l : 0.0f;
+    const RowFactor f(M, m, l);
     uint16_t* out = p.out + (((int64_t)b * c.Hq + hq) * p.n_max + i) * kD + 4 * half;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<uint2*>(out + 32 * j + 2 * e) = make_uint2(row_pack<kBf16>(acc[j][e] * f, acc[j][e + 1] * f),
-                                                                     row_pack<kBf16>(acc[j][e + 2] * f, acc[j][e + 3] * f));
+        *reinterpret_cast<uint2*>(out + 32 * j + 2 * e) = make_uint2(row_pack<kBf16>(f(acc[j][e]), f(acc[j][e + 1])),
+                                                                     row_pack<kBf16>(f(acc[j][e + 2]), f(acc[j][e + 3])));
     return;
   }
   float* rec = p.ws + ((int64_t)first * c.H * p.ntile + ((int64_t)h * p.ntile + tile) * nsplit + split) * (kCols * (kD + 4));

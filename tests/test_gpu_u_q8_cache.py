@@ -775,3 +775,26 @@ def test_empty_rows():
     torch.cuda.synchronize()
     for f, t in c.buffers.items():
         assert torch.equal(t.view(torch.uint8), before[f].view(torch.uint8)), f
+
+
+@pytest.mark.parametrize("n, n_q", [(400, 1), (6000, 1), (400, 150), (6000, 150), (6000, 20)])
+@pytest.mark.parametrize("fmt, e", [("int8", -115), ("int8", -118), ("e4m3", -112), ("e4m3", -115)])
+def test_small_values(fmt, e, n, n_q):
+    """bfloat16 values around 2^e: their scales are above 2^-126 and their means normal numbers, but the factor of the summed
+    products, 2^-7 of a scale over the weights' sum, is not. Splits, the merge and both kernels."""
+    import torch
+    c = _new(1, 1, 2, [n], 64, fmt, "bf16")
+    k = 0.05 * _rows(151, 1, 1, n, 128).double()
+    v = 2.0 ** e * (1 + 0.3 * _rows(152, 1, 1, n, 128).double().clamp(-3, 3))
+    _append(c, 0, k.to(torch.bfloat16), v.to(torch.bfloat16), [0], [n])
+    q = _rows(153, 1, 2, n_q, 128, dtype="bf16")
+    out = _attend(c, [n], q, [n_q], cross=True)
+    a = _numpy(c)
+    assert np.nanmin(a["v_scale"]) > 2.0 ** -126
+    kk, vv = oq.read_sequence(a, 0, 0, 0, n, fmt)
+    for j in range(2):
+        pick = np.unique([0, n_q // 2, n_q - 1])
+        ref, bound = oq.attention(q[0, j, pick].double().numpy(), kk, vv * 2.0 ** -e, np.full(len(pick), n), SM, HALF["bf16"])
+        r = np.abs(out[0, j, pick].double().cpu().numpy() * 2.0 ** -e - ref) / bound
+        _say(f"small values {fmt} 2^{e} {n} tokens rows {n_q} head {j}: worst err / bound {r.max():.3f}")
+        assert r.max() <= 1
