@@ -579,7 +579,9 @@ size_t okvq_q8_workspace_bytes(const okvq_q8_dims* dims, int32_t max_seq_len, in
  *   lens_host   host i32 [B]: lengths with the new tokens (plans the launch; the kernels read seq_lens)
  *   q           device [B][Hq][n_max][128], finite; query head j reads KV head j / G. q and out may be NULL with
  *               n_max 0
- *   n_new_host, n_new_dev  rows of each sequence, 0 <= n_new <= n_max
+ *   n_new_host, n_new_dev  rows of each sequence, 0 <= n_new <= n_max. The host's plan the launch: slots without rows take
+ *               nothing from the others. Where the device has more rows of a slot, those up to the largest n_new_host of
+ *               the call are attended all the same
  *   sm_scale    softmax scale, finite also times log2(e)
  *   out         device [B][Hq][n_max][128] of the rows' type; rows i >= n_new[b] are left as they were
  *   workspace   device, 16-byte aligned, okvq_q8_workspace_bytes(dims, max(lens_host), n_max) bytes

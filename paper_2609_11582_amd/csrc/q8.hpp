@@ -4,13 +4,11 @@
 
 #include "okvq.h"
 #include "okvq_device.hpp"
+#include "q8_plan.hpp"
 
 namespace okvq {
 
 constexpr int kQ8Block = kW * kD;  // bytes of one block of codes: 32 tokens x 128 channels
-constexpr int kQ8MaxBatch = 1024;  // slots: one thread each in the page kernels
-constexpr int kQ8Cols = 16;        // query columns of a tile of the split kernel
-constexpr int kQ8PromptCols = 256; // and of the prompt kernel at most
 
 // ---- rotary --------------------------------------------------------------------------------------
 struct RotaryArgs {
@@ -48,11 +46,6 @@ struct Q8AppendArgs {
 };
 hipError_t launch_q8_append(const Q8AppendArgs& a, int format, int dtype, int B, int blocks, hipStream_t s);
 
-// Splits of each sequence: sequence b has those from first[b] on, up to first[b + 1]; with none there it has one split,
-// which writes the output rows itself
-struct __attribute__((aligned(4))) Q8Splits {
-  uint16_t first[kQ8MaxBatch + 2];  // (read as dwords)
-};
 struct Q8AttendArgs {
   Q8View c;
   const uint16_t* q;
@@ -63,17 +56,8 @@ struct Q8AttendArgs {
   float qscale;  // sm_scale log2(e)
   Q8Splits splits;
 };
-struct Q8Plan {
-  int cols;    // query columns of a tile: rows of a KV head's group, G to a position
-  int ntile;
-  int rows;    // columns that rows have in the first tile
-  int most;    // splits of the sequence that has most
-  Q8Splits splits;
-};
-void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens);
-size_t q8_workspace_bound(int G, int n_max);  // split records of every call of up to n_max rows
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
-hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s);
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s);
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s);
 
 // Page calls, on the whole cache
 struct Q8Pages {
@@ -139,14 +123,6 @@ __device__ __forceinline__ int q8_page(const int32_t* row, int block, const Q8Vi
 // Index of (page, head, block within the page) among the blocks of a layer
 __device__ __forceinline__ int64_t q8_slot(int page, int h, int block, const Q8View& c) {
   return (((int64_t)page * c.H + h) << c.bshift) + (block & ((1 << c.bshift) - 1));
-}
-// first[b] and how many follow, b wave-uniform: two scalar dword loads
-__device__ __forceinline__ int q8_splits(const Q8Splits& s, int b, int* records) {
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(s.first);
-  const uint32_t lo = w[b >> 1], hi = w[(b + 1) >> 1];
-  const int first = (b & 1) ? lo >> 16 : lo & 0xffffu, next = (b & 1) ? hi & 0xffffu : hi >> 16;
-  *records = next - first;
-  return first;
 }
 __device__ __forceinline__ int q8_len(const Q8View& c, int b) {
   return min(max(uniform_load(c.lens + b), 0), c.max_pages << (c.bshift + 5));

@@ -245,11 +245,11 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
   if (most == 0) return OKVQ_OK;
   const int G = d.num_q_heads / d.num_kv_heads;
   Q8Plan plan;
-  q8_plan(plan, d.batch, d.num_kv_heads, G, most, lens_host);
+  q8_plan(plan, d.batch, d.num_kv_heads, G, most, lens_host, n_new_host);
   if (!aligned16(workspace) || workspace_bytes < q8_workspace_bound(G, most)) return OKVQ_ERR_WORKSPACE;
-  if (!launchable((int64_t)plan.most * plan.ntile * d.num_kv_heads * d.batch, 512) ||
-      (plan.most > 1 && (!launchable((int64_t)plan.ntile * d.num_kv_heads * d.batch * 32, 256) ||
-                         (int64_t)plan.ntile * d.num_kv_heads > 65535)))
+  const int64_t units = (int64_t)plan.ntile * d.num_kv_heads;
+  if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
+      (plan.splits.order.most > 1 && (!launchable(units * plan.splits.order.split_slots * 32, 256) || units > 65535)))
     return OKVQ_ERR_UNSUPPORTED;
   Q8AttendArgs a;
   a.c = view(cache, layer);
@@ -261,7 +261,7 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
   a.G = G;
   a.cross = (flags & OKVQ_Q8_CROSS) ? 1 : 0;
   a.qscale = qscale;
-  return hip_status(launch_q8_attention(a, plan, d.format, d.dtype, d.batch, static_cast<hipStream_t>(stream)));
+  return hip_status(launch_q8_attention(a, plan, d.format, d.dtype, static_cast<hipStream_t>(stream)));
 }
 
 size_t okvq_q8_page_workspace_bytes(const okvq_q8_dims* d) {

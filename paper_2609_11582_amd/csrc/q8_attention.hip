@@ -30,8 +30,8 @@ namespace {
 
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kFewRows = 32;                      // rows of a head that always take the split kernel
-constexpr int kRecFloatsQ8 = kQ8Cols * (kD + 4);  // a split's record: [16][128] sums, then [16] of (M, m, l, 0)
+constexpr int kRecFloatsQ8 = kQ8Cols * kQ8Record;  // a split's record: [16][128] sums, then [16] of (M, m, l, 0)
+static_assert(kQ8Record == kD + 4 && kWaves * kW == 256, "as the plan counts");
 constexpr int kCombineRow = kD + 4;               // floats of a combine row: 16 rows of a column fall into all banks
 
 template <int kFmt, bool kBf16>
@@ -39,11 +39,25 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __shared__ __attribute__((aligned(16))) float cmb[kWaves][kQ8Cols * kCombineRow];
   __shared__ float wM[kWaves][kQ8Cols], wm[kWaves][kQ8Cols], wl[kWaves][kQ8Cols];
   const Q8View& c = p.c;
-  const int split = blockIdx.x, h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
+  // everything that says what there is to do, in one wait for the arguments
+  const int layer = blockIdx.z;
+  int ntile = p.ntile;
+  Q8Order order = p.splits.order;
+  uint32_t w = p.splits.part[q8_part_index(layer)], next = p.splits.part[q8_part_index(layer) + 1];
+  __asm__ volatile(""
+                   : "+s"(ntile), "+s"(order.split_slots), "+s"(order.slots), "+s"(order.reordered), "+s"(order.most), "+s"(w), "+s"(next)
+                   : "s"(c.k_codes), "s"(c.table), "s"(c.lens), "s"(c.H), "s"(c.max_pages), "s"(p.q), "s"(p.n_new), "s"(p.n_max), "s"(p.G));
+  const int h = blockIdx.y / ntile, tile = blockIdx.y - h * ntile;
   const int r0 = tile * kQ8Cols;  // first row of the tile
-  int records;
-  const int first = q8_splits(p.splits, b, &records), nsplit = max(records, 1);
-  if (split >= nsplit) return;
+  const int place = q8_place(order, layer, blockIdx.x);
+  const Q8Part mine = q8_part(order, w, next, place, blockIdx.x, tile);
+  if (mine.none) return;
+  int b = place;
+  const int split = mine.split, nsplit = mine.nsplit;
+  if (order.reordered) {
+    b = q8_slot_at(p.splits, place);
+    if (place >= order.active_slots && uniform_load(p.n_new + b) <= 0) return;  // before it loads anything in advance
+  }
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* row = c.table + (int64_t)b * c.max_pages;
@@ -204,13 +218,13 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
     lt += wl[w][cc] * __builtin_amdgcn_exp2f(wm[w][cc] - mt);
     o += *reinterpret_cast<const floatx4*>(&cmb[w][cc * kCombineRow + ch]) * __builtin_amdgcn_exp2f(wM[w][cc] - Mt);
   }
-  if (records == 0) {
+  if (mine.records == 0) {
     const RowFactor f(Mt, mt, lt);
     *reinterpret_cast<uint2*>(p.out + (((int64_t)b * c.Hq + chq) * p.n_max + ci) * kD + ch) =
         make_uint2(row_pack<kBf16>(f(o[0]), f(o[1])), row_pack<kBf16>(f(o[2]), f(o[3])));
     return;
   }
-  float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit + split) * kRecFloatsQ8;
+  float* rec = p.ws + (int64_t)(mine.first * c.H + h * mine.records + tile * nsplit + split) * kRecFloatsQ8;
   *reinterpret_cast<floatx4*>(rec + cc * kD + ch) = o;
   if ((tid & 31) == 0) *reinterpret_cast<floatx4*>(rec + kQ8Cols * kD + 4 * cc) = floatx4{Mt, mt, lt, 0.0f};
 }
@@ -229,17 +243,24 @@ __device__ __forceinline__ float half_reduce(float v, Op&& op) {
 template <bool kBf16, int kGroups, int kCols>
 __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs p, int cols) {
   __shared__ __attribute__((aligned(16))) floatx4 part[kGroups * kCols][32];
-  const int h = blockIdx.y / p.ntile, tile = blockIdx.y - h * p.ntile, b = blockIdx.z;
+  const int place = blockIdx.z;
+  int ntile = p.ntile;
+  Q8Order order = p.splits.order;
+  uint32_t w = p.splits.part[place], next = p.splits.part[place + 1];
+  __asm__ volatile(""  // one wait for them
+                   : "+s"(ntile), "+s"(order.reordered), "+s"(w), "+s"(next)
+                   : "s"(p.ws), "s"(p.n_new), "s"(p.n_max), "s"(p.G), "s"(p.out), "s"(p.c.H), "s"(cols));
+  const int h = blockIdx.y / ntile, tile = blockIdx.y - h * ntile;
   const int tid = threadIdx.x, lane = tid & 31, grp = (tid >> 5) % kGroups, cc = blockIdx.x * kCols + (tid >> 5) / kGroups;
-  int nsplit;
-  const int first = q8_splits(p.splits, b, &nsplit);
-  if (nsplit == 0) return;
+  const Q8Part mine = q8_part(order, w, next, place, 0, tile);
+  if (mine.records == 0) return;
+  const int nsplit = mine.nsplit, b = order.reordered ? q8_slot_at(p.splits, place) : place;
   const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int r = tile * cols + cc, i = r / p.G, hq = h * p.G + (r - i * p.G);
   const bool live = i < n;
   if (kCols == 1 && !live) return;  // the whole work-group
-  const int recf = cols * (kD + 4);
-  const float* rec = p.ws + ((int64_t)first * gridDim.y + (int64_t)blockIdx.y * nsplit) * recf;
+  const int recf = cols * kQ8Record;
+  const float* rec = p.ws + (int64_t)(mine.first * p.c.H + h * mine.records + tile * nsplit) * recf;
   floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   RowFactor factor(kNoScore, kNoScore, 0.0f);
   if (live) {
@@ -290,85 +311,23 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
 
 }  // namespace
 
-// Every split takes the same number of tokens at most, the least that needs no more work-groups than fit the GPU at
-// once: a ragged batch is shared evenly (16 sequences of 8704 to 16384 tokens: 46 -> 41 us against as many splits for each).
-// * The split kernel, 16 columns at a time, up to 32 rows of a head, and up to 112 (7 tiles, each with a read of the cache)
-//   where tokens x heads x tiles are few: 3 positions x 7 heads at 2048 tokens 18.3 -> 9.2 us against the prompt kernel, at
-//   131072 53.5 -> 33.4, 4 positions of 16 sequences at 8192 52.5 -> 48.5; 16 positions at 2048 20.2 -> 10.3, at 32768 28.2 -> 33.0.
-// * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
-//   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
-// * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
-//   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
-// * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
-//   a token (prompts x 28 heads: 64 tokens 12.2 -> 9.3 us, 512 26.0 -> 22.0, 2048 78 -> 72.5; 512 rows against 32768 tokens 322
-//   -> 485, as every work-group widens all codes). Up to 128 rows the second half of the waves only brings tiles, which is
-//   as good (16 tokens 8.4 us, in halves 9.1).
-// * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
-//   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
-void q8_plan(Q8Plan& p, int B, int H, int G, int n_max, const int32_t* lens) {
-  const int64_t rows = (int64_t)n_max * G;
-  int longest = 0;
-  int64_t tokens = 0;
-  for (int b = 0; b < B; ++b) {
-    longest = std::max(longest, lens[b]);
-    tokens += lens[b];
-  }
-  const bool few = rows <= kFewRows || (rows <= 112 && tokens * H * ((rows + kQ8Cols - 1) / kQ8Cols) <= 1 << 18);
-  const bool half = rows > 128 && longest <= 2048 && B * H * ((rows + 255) / 256) <= 256;
-  p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
-  p.ntile = (int)((rows + p.cols - 1) / p.cols);
-  p.rows = (int)std::min<int64_t>(rows, p.cols);
-  const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
-  const int64_t round = few ? kW * kWaves : longest < 4096 ? 512 : 256;  // tokens of a round
-  const int64_t units = (int64_t)H * p.ntile;
-  const auto fits = [&](int64_t rounds) {
-    int64_t n = 0;
-    for (int b = 0; b < B; ++b) n += std::max<int64_t>(1, (lens[b] + rounds * round - 1) / (rounds * round));
-    return n * units <= groups;
-  };
-  int64_t lo = 1, hi = std::max<int64_t>((longest + round - 1) / round, 1);  // hi rounds: one split each
-  if (B * units > groups) lo = hi;
-  while (lo < hi) {  // the fewest rounds that fit
-    const int64_t mid = (lo + hi) / 2;
-    if (fits(mid)) hi = mid;
-    else lo = mid + 1;
-  }
-  if (few && longest <= 4 * round) hi = 4;
-  const bool idle = B * units * 64 < 256 && longest > 64 * 4 * round;
-  const int64_t most = idle ? kQ8MaxSplits : 64;
-  p.most = 1;
-  p.splits.first[0] = 0;
-  for (int b = 0; b < B; ++b) {
-    const int s = (int)std::max<int64_t>(1, std::min((lens[b] + hi * round - 1) / (hi * round), most));
-    p.most = std::max(p.most, s);
-    p.splits.first[b + 1] = (uint16_t)(p.splits.first[b] + (s > 1 ? s : 0));
-  }
-}
-
-// A call's splits fit into its groups, but for units (tiles of a sequence and head) that are more than the groups: those
-// have one split and no record. Calls of few rows and of many count by themselves
-size_t q8_workspace_bound(int G, int n_max) {
-  const size_t few = (size_t)kQ8Groups * kQ8Cols, many = (size_t)kQ8PromptGroups * kQ8PromptCols;
-  return ((int64_t)n_max * G > kFewRows ? std::max(few, many) : few) * (kD + 4) * sizeof(float);
-}
-
 template <int kGroups, int kCols>
-static void merge(const Q8AttendArgs& a, const Q8Plan& p, int B, bool bf16, hipStream_t s) {
+static void merge(const Q8AttendArgs& a, const Q8Plan& p, bool bf16, hipStream_t s) {
   // no work-group for columns that no row has
-  const dim3 grid((p.rows + kCols - 1) / kCols, a.c.H * p.ntile, B), block(32 * kGroups * kCols);
+  const dim3 grid((p.rows + kCols - 1) / kCols, a.c.H * p.ntile, p.splits.order.split_slots), block(32 * kGroups * kCols);
   if (bf16) hipLaunchKernelGGL((k_q8_merge<true, kGroups, kCols>), grid, block, 0, s, a, p.cols);
   else hipLaunchKernelGGL((k_q8_merge<false, kGroups, kCols>), grid, block, 0, s, a, p.cols);
 }
 
-hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s) {
   a.ntile = p.ntile;
   a.splits = p.splits;
   const bool bf16 = dtype == OKVQ_BF16;
   hipError_t e;
   if (p.cols != kQ8Cols) {
-    e = launch_q8_prompt(a, p, format, dtype, B, s);
+    e = launch_q8_prompt(a, p, format, dtype, s);
   } else {
-    const dim3 grid(p.most, a.c.H * p.ntile, B), block(kThreads);
+    const dim3 grid(p.splits.order.most, a.c.H * p.ntile, q8_layers(p)), block(kThreads);
     if (format == OKVQ_Q8_INT8) {
       if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
       else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
@@ -378,12 +337,12 @@ hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int
     }
     e = hipGetLastError();
   }
-  if (e != hipSuccess || p.most == 1) return e;
+  if (e != hipSuccess || p.splits.order.most == 1) return e;
   // a column to 8 groups of lanes, 16 where there are many splits (128 splits: 7.9 -> 4.5 us); 8 columns to a work-group
   // where there are few (2 splits of 32768 rows: 33 -> 8 us)
-  if (p.most > 64) merge<16, 1>(a, p, B, bf16, s);
-  else if (p.most > 8 || p.cols == kQ8Cols) merge<8, 1>(a, p, B, bf16, s);
-  else merge<1, 8>(a, p, B, bf16, s);
+  if (p.splits.order.most > 64) merge<16, 1>(a, p, bf16, s);
+  else if (p.splits.order.most > 8 || p.cols == kQ8Cols) merge<8, 1>(a, p, bf16, s);
+  else merge<1, 8>(a, p, bf16, s);
   return hipGetLastError();
 }
 

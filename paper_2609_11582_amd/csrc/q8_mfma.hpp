@@ -14,9 +14,6 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr float kNoScore = -1e30f;   // a reference before any token; finite, so that differences with -inf are -inf
 constexpr float kLazy = 8.0f;        // references move when passed by 2^8
 constexpr float kWeightExp = 7.0f;   // weights are at most 2^(kLazy + kWeightExp)
-constexpr int kQ8MaxSplits = 128;
-constexpr int kQ8Groups = 512;       // work-groups that a call of few rows is split into
-constexpr int kQ8PromptGroups = 256; // and a call of many: one for each compute unit
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const half2v v = {(_Float16)lo, (_Float16)hi};

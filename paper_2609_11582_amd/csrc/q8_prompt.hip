@@ -33,20 +33,26 @@ struct Raw {                              // a thread's 16 bytes of keys or of v
 };
 
 template <int kFmt, bool kBf16, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, int B) {
+__global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, int width) {
   constexpr int kCols = 32 * kWaves, kPieces = 8 / kWaves;
   // two buffers of keys [block][16 channels][half h, token: at token ^ (channels & 7)] and of values
   // [block][32 channels][step s][half h, channel], as operands; the scales of three tiles, as the keys are ahead
   __shared__ uint4 kbuf[2][2][8][kOperand], vbuf[2][2][4][2][kOperand];
   __shared__ float kscale[3][2], vscale[2][2];
   const Q8View& c = p.c;
-  // sequences and heads vary fastest: work-groups go round the 8 XCDs, so a head's tiles meet in few L2s; the last rows,
-  // which see most, start first
-  const int units = B * c.H, unit = blockIdx.x % units, split = blockIdx.y;
-  const int tile = p.ntile - 1 - (int)(blockIdx.x / units), b = unit / c.H, h = unit - b * c.H;
-  int records;
-  const int first = q8_splits(p.splits, b, &records), nsplit = max(records, 1);
-  if (split >= nsplit) return;
+  Q8Order order = p.splits.order;
+  int ntile = p.ntile;
+  __asm__ volatile(""  // one wait for the arguments
+                   : "+s"(order.split_slots), "+s"(order.active_slots), "+s"(order.slots), "+s"(order.reordered), "+s"(ntile)
+                   : "s"(c.k_codes), "s"(c.table), "s"(c.lens), "s"(c.max_pages), "s"(p.n_new), "s"(p.n_max), "s"(p.G), "s"(c.H));
+  const Q8Tile at = q8_tile(order, c.H, ntile, width, blockIdx.x, blockIdx.y);
+  if (at.place < 0) return;
+  const int tile = at.tile, h = at.h;
+  Q8Part mine;
+  if (at.place < order.split_slots) mine = q8_part(order, p.splits.part[at.place], p.splits.part[at.place + 1], at.place, blockIdx.y, tile);
+  else mine.none = false;
+  if (mine.none) return;
+  const int b = order.reordered ? q8_slot_at(p.splits, at.place) : at.place, split = mine.split, nsplit = mine.nsplit;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + (int64_t)b * c.max_pages;
@@ -62,8 +68,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   const int wave_first = (r0 + 32 * wave) / p.G;
   const int vis_first = wave_first >= n ? 0 : p.cross ? len : max(len - n + wave_first + 1, 0);
   const bool busy = wave_first < n;  // a wave without a live column has only its part of the tiles to bring
-  const int ntile = (vis_last + kTile - 1) / kTile;
-  const int per = (ntile + nsplit - 1) / nsplit, t_begin = min(split * per, ntile), t_end = min(t_begin + per, ntile);
+  const int steps = (vis_last + kTile - 1) / kTile;
+  const int per = (steps + nsplit - 1) / nsplit, t_begin = min(split * per, steps), t_end = min(t_begin + per, steps);
 
   // Staging: a thread has 16 bytes of key row tid / 8 % 32 and of value slot tid % 256 of kPieces of the tile's two blocks.
   // Behind the sequence its last block stands for those to come: what a zero weight multiplies has to be finite. Values
@@ -290,7 +296,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
 
   l = sum32(l);
   if (!live) return;
-  if (records == 0) {
+  if (mine.records == 0) {
     const RowFactor f(M, m, l);
     uint16_t* out = p.out + (((int64_t)b * c.Hq + hq) * p.n_max + i) * kD + 4 * half;
 #pragma unroll
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
                                                                      row_pack<kBf16>(f(acc[j][e + 2]), f(acc[j][e + 3])));
     return;
   }
-  float* rec = p.ws + ((int64_t)first * c.H * p.ntile + ((int64_t)h * p.ntile + tile) * nsplit + split) * (kCols * (kD + 4));
+  float* rec = p.ws + (int64_t)(mine.first * c.H + h * mine.records + tile * nsplit + split) * (kCols * kQ8Record);
   const int cc = 32 * wave + col;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -315,15 +321,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
 }  // namespace
 
 template <int kFmt, bool kBf16>
-static void launch(const Q8AttendArgs& a, const Q8Plan& p, int B, hipStream_t s) {
-  const dim3 grid((unsigned)(B * a.c.H * p.ntile), p.most);
-  if (p.cols == 256) hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 8>), grid, dim3(512), 0, s, a, B);
-  else hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 4>), grid, dim3(256), 0, s, a, B);
+static void launch(const Q8AttendArgs& a, const Q8Plan& p, hipStream_t s) {
+  const int width = q8_layers(p) * a.c.H * p.ntile;
+  const dim3 grid((unsigned)width, p.splits.order.most);
+  if (p.cols == 256) hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 8>), grid, dim3(512), 0, s, a, width);
+  else hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 4>), grid, dim3(256), 0, s, a, width);
 }
 
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, int B, hipStream_t s) {
-  if (format == OKVQ_Q8_INT8) dtype == OKVQ_BF16 ? launch<OKVQ_Q8_INT8, true>(a, p, B, s) : launch<OKVQ_Q8_INT8, false>(a, p, B, s);
-  else dtype == OKVQ_BF16 ? launch<OKVQ_Q8_E4M3, true>(a, p, B, s) : launch<OKVQ_Q8_E4M3, false>(a, p, B, s);
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s) {
+  if (format == OKVQ_Q8_INT8) dtype == OKVQ_BF16 ? launch<OKVQ_Q8_INT8, true>(a, p, s) : launch<OKVQ_Q8_INT8, false>(a, p, s);
+  else dtype == OKVQ_BF16 ? launch<OKVQ_Q8_E4M3, true>(a, p, s) : launch<OKVQ_Q8_E4M3, false>(a, p, s);
   return hipGetLastError();
 }
 

@@ -798,3 +798,64 @@ def test_small_values(fmt, e, n, n_q):
         r = np.abs(out[0, j, pick].double().cpu().numpy() * 2.0 ** -e - ref) / bound
         _say(f"small values {fmt} 2^{e} {n} tokens rows {n_q} head {j}: worst err / bound {r.max():.3f}")
         assert r.max() <= 1
+
+
+@pytest.mark.parametrize("n_q", [1, 4, 90])
+@pytest.mark.parametrize("parked", [0, 700])
+def test_idle_slots_take_no_part(n_q, parked):
+    """One sequence with new rows in a cache of 64 slots, the others empty or parked: it is attended as in a cache of its own
+    (bit for bit: the same splits), and the other slots' rows are left as they were."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B, H, Hq, n, at = 64, 4, 16, 20000, 37
+    lens = [parked] * B
+    lens[at] = n
+    c = _new(B, H, Hq, lens, 256, "int8", "fp16", seed=161)
+    k, v = _rows(162, 1, H, n, 128), _rows(163, 1, H, n, 128)
+    alone = dict(c.buffers, block_table=c["block_table"][at:at + 1].clone(), seq_lens=_i32([n]),
+                 k_stage=torch.zeros(1, 1, H, 32, 128, dtype=torch.float16, device="cuda"),
+                 v_stage=torch.zeros(1, 1, H, 32, 128, dtype=torch.float16, device="cuda"))
+    c1 = okvq.Q8Cache(1, H, Hq, c.dims.num_pages, c.dims.max_pages, page_tokens=256, buffers=alone)
+    _append(c1, 0, k, v, [0], [n])
+    c["seq_lens"].copy_(_i32(lens))
+    q = torch.full((B, Hq, n_q, 128), float("nan"), dtype=torch.float16)
+    q[at] = _rows(164, Hq, n_q, 128)
+    new = [n_q if b == at else 0 for b in range(B)]
+    want = _attend(c1, [n], q[at:at + 1], [n_q])
+    out = _attend(c, lens, q, new)
+    assert torch.equal(out[at], want[0])
+    assert bool((out[torch.arange(B) != at] == 9).all())
+    a = _numpy(c1)
+    ref, bound = oq.attention(q[at, 0, -1:].double().numpy(), *oq.read_sequence(a, 0, 0, 0, n, "int8"), np.array([n]), SM, HALF["fp16"])
+    assert np.all(np.abs(want[0, 0, -1:].double().cpu().numpy() - ref) <= bound)
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("H, Hq, lens, new", [
+    (1, 7, [5000, 3000, 2000, 40, 0, 6000], [300, 1, 1, 0, 0, 1]),       # a chunk beside single tokens
+    (2, 8, [9000, 50, 60, 0, 70, 30, 20, 8000], [2, 1, 3, 0, 1, 0, 1, 1]),
+    (4, 16, [20, 4000, 700], [20, 3, 700]),
+])
+def test_uneven_counts(fmt, dtype, H, Hq, lens, new):
+    B, n = len(lens), max(new)
+    c = _filled(B, H, Hq, lens, 64, fmt, dtype, 171)
+    q = _rows(172, B, Hq, n, 128, dtype=dtype)
+    out = _attend(c, lens, q, new)
+    _check_attention(c, out, lens, q, new, fmt, dtype, f"uneven counts {fmt} {lens} {new}", rows=np.array([0, 1, 19, 150, 299, 699]))
+
+
+def test_rows_that_the_host_did_not_count():
+    """A captured call's host counts are those of the capture: slots that have rows on the device alone, or more of them than
+    the host said (up to the call's largest count), are attended too."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    lens, n = [6000, 900, 40, 5000], 40
+    for Hq in (2, 8):  # split kernel and prompt kernel
+        c = _filled(4, 2, Hq, lens, 64, "int8", "fp16", 181)
+        q = _rows(182, 4, Hq, n, 128)
+        for planned, real in (([1, 0, 0, 40], [1, 1, 40, 3]), ([40, 0, 0, 0], [0, 40, 30, 40]), ([5, 40, 1, 0], [40, 0, 40, 40])):
+            out = torch.full(q.shape, 9.0, dtype=torch.float16, device="cuda")
+            okvq.okvq_q8_attention(c, 0, lens, q.cuda(), planned, _i32(real), n, SM, out, okvq.q8_workspace(c.dims, 6000, n))
+            _check_attention(c, out, lens, q, real, "int8", "fp16", f"planned {planned}, real {real}", rows=np.array([0, 20, 39]))
