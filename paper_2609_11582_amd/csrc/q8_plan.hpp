@@ -114,6 +114,10 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 //   as good (16 tokens 8.4 us, in halves 9.1).
 // * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
 //   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
+// * Where the tiles alone are more than the GPU holds at once, one split each; but sequences of more than twice the mean work of
+//   a place are split into such means, as far as there are records (4 heads, one token: 200 sequences of 300 tokens and one of
+//   131072 627 -> 38.5 us, 200 spread over 64 to 16384 176 -> 132). From the mean itself on, 200 of 2000 and one of 4096
+//   81.7 -> 85.7, 200 even up to 16000 354 -> 348.
 // most_new: the most new rows of a slot, 1 at least.
 inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new) {
   const int64_t rows = (int64_t)most_new * G;
@@ -143,14 +147,21 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     units = 0;
     for (int b = 0; b < B; ++b) units += tiles(b, p.cols) * H;
   }
-  const auto fits = [&](int64_t rounds) {
+  const bool over = units > groups;
+  const auto count = [&](int64_t rounds, bool all) {  // work-groups of splits of so many rounds, or those that have a record
     int64_t n = 0;
-    for (int b = 0; b < B; ++b)
-      if (n_new[b] > 0) n += std::max<int64_t>(1, (lens[b] + rounds * round - 1) / (rounds * round)) * tiles(b, p.cols) * H;
-    return n <= groups;
+    for (int b = 0; b < B; ++b) {
+      const int64_t s = n_new[b] > 0 ? std::max<int64_t>(1, (lens[b] + rounds * round - 1) / (rounds * round)) : 0;
+      if (all || s > 1) n += s * tiles(b, p.cols) * H;
+    }
+    return n;
   };
+  const auto fits = [&](int64_t rounds) { return count(rounds, !over) <= groups; };
   int64_t lo = 1, hi = std::max<int64_t>((longest + round - 1) / round, 1);  // hi rounds: one split each
-  if (units > groups) lo = hi;
+  if (over) {
+    const int64_t mean = (count(1, true) + groups - 1) / groups;
+    lo = hi > 2 * mean ? mean : hi;
+  }
   while (lo < hi) {  // the fewest rounds that fit
     const int64_t mid = (lo + hi) / 2;
     if (fits(mid)) hi = mid;

@@ -88,5 +88,14 @@ int main() {
         std::memcmp(q.splits.part, p.splits.part, 4 * (p.splits.order.split_slots + 1)) != 0)
       fail("idle slots change the plan", B, H, G, lens, n_new);
   }
+  // a long sequence among more short ones than the GPU holds at once
+  for (const int B : {200, 1000})
+    for (const int rows : {1, 30}) {
+      std::vector<int32_t> lens(B, 300), n_new(B, rows);
+      lens[B / 3] = 131072;
+      Q8Plan p;
+      q8_plan(p, B, 4, 7, rows, lens.data(), n_new.data());
+      if (p.splits.order.split_slots != 1 || p.splits.order.most < 10) fail("a long sequence is not split", B, 4, 7, lens, n_new);
+    }
   std::printf("ok\n");
 }

@@ -859,3 +859,29 @@ def test_rows_that_the_host_did_not_count():
             out = torch.full(q.shape, 9.0, dtype=torch.float16, device="cuda")
             okvq.okvq_q8_attention(c, 0, lens, q.cuda(), planned, _i32(real), n, SM, out, okvq.q8_workspace(c.dims, 6000, n))
             _check_attention(c, out, lens, q, real, "int8", "fp16", f"planned {planned}, real {real}", rows=np.array([0, 20, 39]))
+
+
+@pytest.mark.parametrize("n_q", [1, 20])
+def test_a_long_sequence_among_many_short_ones(n_q):
+    """More short sequences than the GPU holds at once, and a long one that is split all the same."""
+    import torch
+    B, H, Hq, at = 200, 3, 12, 70
+    lens = [20 + 7 * (b % 5) for b in range(B)]
+    lens[at] = 30000
+    c = _new(B, H, Hq, lens, 64, "int8", "fp16", seed=191)
+    g = torch.Generator(device="cuda").manual_seed(192)
+    for f in ("k_codes", "v_codes"):
+        c[f].random_(0, 256, generator=g)
+    c["k_scale"].uniform_(0.005, 0.01, generator=g)
+    c["v_scale"].uniform_(0.01, 0.04, generator=g)
+    c["seq_lens"].copy_(_i32(lens))
+    q = _rows(193, B, Hq, n_q, 128)
+    out = _attend(c, lens, q, [n_q] * B).double().cpu().numpy()
+    a = _numpy(c)
+    for b in (0, 1, at - 1, at, at + 1, B - 1):
+        for h in range(H):
+            k, v = oq.read_sequence(a, 0, b, h, lens[b], "int8")
+            for j in range(h * Hq // H, (h + 1) * Hq // H):
+                ref, bound = oq.attention(q[b, j].double().numpy(), k, v, lens[b] - n_q + np.arange(n_q) + 1, SM, HALF["fp16"])
+                assert np.all(np.abs(out[b, j] - ref) <= bound), (b, j)
+    assert np.isfinite(out).all()
