@@ -74,20 +74,26 @@ __device__ int list_pages(const Q8Pages& c, int lo, int hi, bool used, int most,
   return min(found, most);
 }
 
-// Copies of the list, in units of one layer's kCopyBytes of one page's codes, by groups of kCopyThreads threads; the
-// scales of a page go with its first unit
-__device__ __forceinline__ void copy_pages(const Q8Pages& c, const int32_t* pairs, int copies, int group, int groups, int tid) {
+// Copies of the plan, in units of one layer's kCopyBytes of one page's codes; the scales of a page go with its first unit. Of a
+// compaction (places) also every table entry becomes its page's new place, ws.list
+__global__ __launch_bounds__(kCopyThreads) void k_q8_copy(Q8Pages c, Q8PageWs ws, bool places) {
+  const int tid = threadIdx.x;
+  if (places)
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + tid; i < (int64_t)c.B * c.max_pages; i += (int64_t)gridDim.x * kCopyThreads) {
+      const int id = c.table[i];
+      if (id >= 0 && id < c.P) c.table[i] = ws.list[id];
+    }
   const int64_t page_bytes = (int64_t)c.H * c.T * kD;  // of one kind
   const int scales = c.H * (c.T / kW);
   const int per = (int)((page_bytes + kCopyBytes - 1) / kCopyBytes);
-  const int64_t units = (int64_t)copies * c.L * 2 * per;
-  for (int64_t u = group; u < units; u += groups) {
+  const int64_t units = (int64_t)ws.count[0] * c.L * 2 * per;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int part = (int)(u % per);
     int64_t v = u / per;
     const bool values = v & 1;
     v >>= 1;
     const int layer = (int)(v % c.L), pair = (int)(v / c.L);
-    const int64_t from = (int64_t)layer * c.P + pairs[2 * pair], to = (int64_t)layer * c.P + pairs[2 * pair + 1];
+    const int64_t from = (int64_t)layer * c.P + ws.pairs[2 * pair], to = (int64_t)layer * c.P + ws.pairs[2 * pair + 1];
     uint8_t* codes = values ? c.v_codes : c.k_codes;
     const uint4* src = reinterpret_cast<const uint4*>(codes + from * page_bytes);
     uint4* dst = reinterpret_cast<uint4*>(codes + to * page_bytes);
@@ -106,20 +112,7 @@ __device__ __forceinline__ void copy_pages(const Q8Pages& c, const int32_t* pair
   }
 }
 
-// Copies of the plan; of a compaction (places) also every table entry becomes its page's new place, ws.list
-__global__ __launch_bounds__(kCopyThreads) void k_q8_copy(Q8Pages c, Q8PageWs ws, bool places) {
-  if (places)
-    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < (int64_t)c.B * c.max_pages;
-         i += (int64_t)gridDim.x * kCopyThreads) {
-      const int id = c.table[i];
-      if (id >= 0 && id < c.P) c.table[i] = ws.list[id];
-    }
-  copy_pages(c, ws.pairs, ws.count[0], blockIdx.x, gridDim.x, threadIdx.x);
-}
-
-// copy_here: the plan's work-group makes the copies too
-__global__ __launch_bounds__(kPlan) void k_q8_extend(Q8Pages c, const int32_t* n_new, int32_t* granted, Q8PageWs ws,
-                                                     bool copy_here) {
+__global__ __launch_bounds__(kPlan) void k_q8_extend(Q8Pages c, const int32_t* n_new, int32_t* granted, Q8PageWs ws) {
   __shared__ int scratch[kWaves + 1];
   __shared__ int last_of[kPlan], start_of[kPlan + 1], first_of[kPlan];
   __shared__ int bad, copies;
@@ -191,10 +184,7 @@ __global__ __launch_bounds__(kPlan) void k_q8_extend(Q8Pages c, const int32_t* n
     granted[b] = n;
   }
   __syncthreads();
-  if (copy_here)
-    copy_pages(c, ws.pairs, copies, b / kCopyThreads, kPlan / kCopyThreads, b % kCopyThreads);
-  else if (b == 0)
-    ws.count[0] = copies;
+  if (b == 0) ws.count[0] = copies;
 }
 
 __device__ void let_go(const Q8Pages& c, int b) {
@@ -297,12 +287,12 @@ Q8PageWs q8_page_ws(void* ws, int B, int P) {
 
 hipError_t launch_q8_extend(const Q8Pages& c, const int32_t* n_new, int32_t* granted, void* ws, hipStream_t s) {
   const Q8PageWs w = q8_page_ws(ws, c.B, c.P);
-  // Copies of at most 256 KB (every slot at once, which is rare) are made by the plan's work-group: 8 steps of 4 sequences of
-  // one layer, each with its rotary, append and attention, 300 us without the second launch, 314 with it
-  const bool copy_here = (int64_t)c.B * c.L * 2 * c.H * c.T * kD <= 256 << 10;
-  hipLaunchKernelGGL(k_q8_extend, dim3(1), dim3(kPlan), 0, s, c, n_new, granted, w, copy_here);
+  hipLaunchKernelGGL(k_q8_extend, dim3(1), dim3(kPlan), 0, s, c, n_new, granted, w);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || copy_here) return e;
+  if (e != hipSuccess) return e;
+  // A launch of 1.5 us (4.4 instead of 2.8 us a call) where no slot copies, which the host cannot know. In the plan's
+  // work-group copies are as fast up to some 100 KB only (4 slots x 4 heads x 32 tokens of one layer 9.9 us against 9.5, of 64
+  // tokens 12.2 against 9.9, 28 layers 155 against 22): no cache of several layers has so little to copy
   return launch_copy(c, w, c.B, false, s);
 }
 
