@@ -101,9 +101,12 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 // Only the slots with new rows count, each with the tiles that its own rows take (one token at 32768 in a cache of 64 slots
 // without other rows 71 -> 11.8 us, of 1024 178 -> 14.6; 512 rows in one of 16 slots 1820 -> 257; 512 rows beside 15 single tokens
 // at 8192 914 -> 245).
-// * The split kernel, 16 columns at a time, up to 32 rows of a head, and up to 112 (7 tiles, each with a read of the cache)
-//   where tokens x heads x tiles are few: 3 positions x 7 heads at 2048 tokens 18.3 -> 9.2 us against the prompt kernel, at
-//   131072 53.5 -> 33.4, 4 positions of 16 sequences at 8192 52.5 -> 48.5; 16 positions at 2048 20.2 -> 10.3, at 32768 28.2 -> 33.0.
+// * The split kernel, 16 columns at a time, up to 32 rows of a head (0.47 to 1.0 of the prompt kernel's time in 97 of 105 calls,
+//   1.12 at most, 64 sequences of 2000), and beyond where all its tiles find a place at once and tiles x tokens, its reads of
+//   the cache, are few: in 390 calls of 113 to 8192 rows within both bounds it takes 0.36 to 0.84 of the prompt kernel's time
+//   (16 positions x 7 heads at 1024 tokens 18.5 -> 9.4 us, a prompt of 100 x 28 heads 11 -> 5.9). With 640 work-groups it
+//   takes up to 1.11, with 1152 1.57 (16 prompts of 40), at 2^18.6 tile tokens 1.16 (4 sequences of 2048, 8 heads, 84 rows), at
+//   2^19.6 1.6 (16 sequences of 8192, 1 head, 84 rows: 38 us against 23.6).
 // * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
 //   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
@@ -128,14 +131,12 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     if (n_new[b] == 0) continue;
     ++active;
     longest = std::max(longest, lens[b]);
-    if (rows <= 112) {
-      const int64_t n = rows <= kQ8Cols ? H : tiles(b, kQ8Cols) * H;
-      units16 += n;
-      work16 += n * lens[b];
-    }
+    const int64_t n = rows <= kQ8Cols ? H : tiles(b, kQ8Cols) * H;
+    units16 += n;
+    work16 += n * lens[b];
     if (rows > kFewRows) units256 += tiles(b, kQ8PromptCols) * H;
   }
-  const bool few = rows <= kFewRows || (rows <= 112 && work16 <= 1 << 18);
+  const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18);
   const bool half = rows > 128 && longest <= 2048 && units256 <= 256;
   p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);

@@ -885,3 +885,59 @@ def test_a_long_sequence_among_many_short_ones(n_q):
                 ref, bound = oq.attention(q[b, j].double().numpy(), k, v, lens[b] - n_q + np.arange(n_q) + 1, SM, HALF["fp16"])
                 assert np.all(np.abs(out[b, j] - ref) <= bound), (b, j)
     assert np.isfinite(out).all()
+
+
+@pytest.mark.parametrize("n", [700, 2500])
+@pytest.mark.parametrize("kind, fmt, dtype", [
+    ("causal", "int8", "fp16"), ("causal", "e4m3", "bf16"), ("cross", "int8", "bf16"), ("few tokens", "e4m3", "fp16"), ("negative", "int8", "fp16"),
+    ("flat", "e4m3", "bf16"), ("dominant", "int8", "fp16"), ("dominant", "e4m3", "fp16"), ("zero blocks", "int8", "fp16"),
+    ("zero blocks", "e4m3", "fp16"), ("far scales", "int8", "bf16"), ("far scales", "e4m3", "bf16"), ("small values", "int8", "bf16"),
+    ("small values", "e4m3", "bf16")])
+def test_many_rows_of_many_heads(kind, fmt, dtype, n):
+    """Calls of more tiles than the split kernel takes (300 rows x 16 heads of 2 KV heads), with 128 and with 256 columns."""
+    import torch
+    H, Hq, n_q, cross, sm, unit = 2, 32, 300, kind in ("cross", "small values"), SM, 0
+    g = torch.Generator().manual_seed(211)
+    k, v = 0.1 * torch.randn(1, H, n, 128, generator=g).double(), torch.randn(1, H, n, 128, generator=g).double()
+    q = torch.randn(1, Hq, n_q, 128, generator=g).double()
+    lens, block = [n], torch.arange(n) // 32
+    if kind == "few tokens":     # more rows than tokens: the first ones see nothing
+        lens, k, v = [130], k[:, :, :130], v[:, :, :130]
+    elif kind == "negative":
+        sm = -1.5
+    elif kind == "flat":
+        sm = 0.0
+    elif kind in ("dominant", "zero blocks"):
+        q[:, ::2] = 0.0
+        q[:, ::2, :, 0] = math.log(2.0) / SM  # scores of every other head are the first channel, in log2 units
+        v *= 1e-2
+        if kind == "dominant":
+            at = torch.arange(5, n, 150)
+            k[0, :, at, 0] = torch.linspace(10, 30, len(at)).double()
+            v *= torch.where(torch.arange(n) % 150 < 32, 2.0 ** -9, 8.0)[:, None]
+        else:
+            k[:, :, 32:64, 0] += 8.0
+            v[:, :, 32:64] = 0.0
+            v[:, :, 320:352] = -0.0
+    elif kind == "far scales":
+        unit = 75
+        v *= torch.where(block % 3 == 1, 2.0 ** 75, 2.0 ** -75)[:, None]
+    elif kind == "small values":
+        unit = -115
+        v = 2.0 ** -115 * (1 + 0.3 * v.clamp(-3, 3))
+    c = _new(1, H, Hq, lens, 64, fmt, dtype, seed=212)
+    k, v, q = (x.to(c.row_dtype) for x in (k, v, q))
+    _append(c, 0, k, v, [0], lens)
+    out = _attend(c, lens, q, [n_q], cross, sm)
+    a, got = _numpy(c), out.double().cpu().numpy() * 2.0 ** -unit
+    assert np.isfinite(got).all()
+    pick = np.array([0, 1, 150, 169, 170, 171, 299])
+    seen = np.full(len(pick), lens[0]) if cross else lens[0] - n_q + pick + 1
+    worst = 0.0
+    for j in range(Hq):
+        kk, vv = oq.read_sequence(a, 0, 0, j // 16, lens[0], fmt)
+        ref, bound = oq.attention(q[0, j, pick].double().numpy(), kk, vv * 2.0 ** -unit, seen, sm, HALF[dtype])
+        assert np.all(got[0, j, pick][seen <= 0] == 0)
+        worst = max(worst, float((np.abs(got[0, j, pick] - ref) / np.maximum(bound, 1e-30)).max()))
+    _say(f"many rows of many heads, {kind} {fmt} {dtype} {n}: worst err / bound {worst:.3f}")
+    assert worst <= 1
