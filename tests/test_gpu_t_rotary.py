@@ -211,3 +211,26 @@ def test_far_positions_of_high_frequencies(sign):
     err = np.abs(out.double().cpu().numpy() - ref) / (HALF["fp16"] * np.abs(ref) + 2.0 ** -21 * size + 2.0 ** -25)
     print(f"[gpu-case] far positions of high frequencies: worst err / tolerance {err.max():.3f}", flush=True)
     assert err.max() <= 1
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("inverse", [False, True])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("lens", [[1285], [1003, 0, 517, 8, 1], [7] * 200])
+def test_many_tokens(dtype, inverse, adjacent, lens):
+    """Enough tokens for work-groups of eight (more than 1280 in a launch), of ragged lengths; rows behind them stay."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    B, n, hq, hk = len(lens), max(lens), 5, 1
+    q, pos = _inputs(B, hq, n, dtype, 21)
+    k, _ = _inputs(B, hk, n, dtype, 22)
+    flags = (okvq.OKVQ_ROTARY_INVERSE if inverse else 0) | (okvq.OKVQ_ROTARY_ADJACENT if adjacent else 0)
+    qo, ko = (torch.full((B, h, n, 128), 5.0, dtype=q.dtype, device="cuda") for h in (hq, hk))
+    okvq.okvq_rotary(okvq.make_rotary(FREQ, AXES), q.cuda().transpose(1, 2), k.cuda().transpose(1, 2), pos.cuda(), qo, ko, lens=lens, flags=flags)
+    for x, y in ((q, qo), (k, ko)):
+        for b, m in enumerate(lens):
+            assert bool((y[b, :, m:] == 5).all())
+            if m and (b < 5 or b == B - 1):
+                _check(y[b:b + 1, :, :m].double().cpu().numpy(), x[b:b + 1, :m].transpose(1, 2).double().numpy(), pos[b:b + 1, :, :m].numpy(), dtype,
+                       f"sequence {b} of {m}", inverse=inverse, adjacent=adjacent)
