@@ -570,8 +570,8 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
                            void* stream);
 
 /* Device workspace bytes that okvq_q8_attention needs for sequences up to max_seq_len and up to n_max rows
- * (0 for invalid arguments). Enough for every shorter call too. No initial contents are needed; calls that
- * may overlap, captured graphs among them, need one each. */
+ * (0 for invalid arguments). Enough for every shorter call too (up to 32 rows of a KV head 4.3 MB, beyond 34.6 MB, whatever the
+ * lengths). No initial contents are needed; calls that may overlap, captured graphs among them, need one each. */
 size_t okvq_q8_workspace_bytes(const okvq_q8_dims* dims, int32_t max_seq_len, int32_t n_max);
 
 /* Attention of new rows over one layer of the 8-bit cache: one token a sequence (a decode step: the

@@ -74,14 +74,12 @@ Q8Pages pages(const okvq_q8_cache* c) {
 }
 
 // lens_host and n_new_host of a call; n_new may exceed the length where a row may see nothing (empty_rows)
-okvq_status check_rows(const okvq_q8_dims& d, const int32_t* lens, const int32_t* n_new, int32_t n_max, bool empty_rows,
-                       int* max_len, int* most) {
-  *max_len = *most = 0;
+okvq_status check_rows(const okvq_q8_dims& d, const int32_t* lens, const int32_t* n_new, int32_t n_max, bool empty_rows, int* most) {
+  *most = 0;
   for (int b = 0; b < d.batch; ++b) {
     if (lens[b] < 0 || n_new[b] < 0 || n_new[b] > n_max) return OKVQ_ERR_INVALID_ARGUMENT;
     if (lens[b] > capacity(d)) return OKVQ_ERR_CAPACITY;
     if (!empty_rows && n_new[b] > lens[b]) return OKVQ_ERR_INVALID_ARGUMENT;
-    *max_len = std::max(*max_len, lens[b]);
     *most = std::max(*most, n_new[b]);
   }
   return OKVQ_OK;
@@ -222,8 +220,8 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
   const okvq_q8_dims& d = cache->dims;
   if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0) return OKVQ_ERR_INVALID_ARGUMENT;
   if (!rows_at(k_new, n_max) || !rows_at(v_new, n_max) || !aligned16(n_new_dev)) return OKVQ_ERR_INVALID_ARGUMENT;
-  int max_len, most;
-  st = check_rows(d, lens_host, n_new_host, n_max, false, &max_len, &most);
+  int most;
+  st = check_rows(d, lens_host, n_new_host, n_max, false, &most);
   if (st != OKVQ_OK) return st;
   if (most == 0) return OKVQ_OK;
   // blocks that `most` tokens can touch wherever the sequence ends: the lengths on the device decide which
@@ -249,11 +247,13 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
       (flags & ~(uint32_t)OKVQ_Q8_CROSS))
     return OKVQ_ERR_INVALID_ARGUMENT;
   if (!rows_at(q, n_max) || !aligned16(n_new_dev) || !rows_at(out, n_max)) return OKVQ_ERR_INVALID_ARGUMENT;
-  int max_len, most;
-  st = check_rows(d, lens_host, n_new_host, n_max, true, &max_len, &most);
+  int most;
+  st = check_rows(d, lens_host, n_new_host, n_max, true, &most);
   if (st != OKVQ_OK) return st;
   if (most == 0) return OKVQ_OK;
   const int G = d.num_q_heads / d.num_kv_heads;
+  // before the plan, whose products stay inside 64 bits for what can be launched
+  if (!launchable(((int64_t)most * G + kQ8PromptCols - 1) / kQ8PromptCols * d.num_kv_heads, 512)) return OKVQ_ERR_UNSUPPORTED;
   Q8Plan plan;
   q8_plan(plan, d.batch, d.num_kv_heads, G, most, lens_host, n_new_host);
   if (!aligned16(workspace) || workspace_bytes < q8_workspace_bound(G, most)) return OKVQ_ERR_WORKSPACE;

@@ -122,6 +122,7 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 //   131072 627 -> 38.5 us, 200 spread over 64 to 16384 176 -> 132). From the mean itself on, 200 of 2000 and one of 4096
 //   81.7 -> 85.7, 200 even up to 16000 354 -> 348.
 // most_new: the most new rows of a slot, 1 at least.
+// Tiles of 256 columns x heads are below 2^23 a slot (checked before), so that no product here passes 64 bits.
 inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new) {
   const int64_t rows = (int64_t)most_new * G;
   const auto tiles = [&](int b, int cols) { return ((int64_t)n_new[b] * G + cols - 1) / cols; };
@@ -133,7 +134,7 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     longest = std::max(longest, lens[b]);
     const int64_t n = rows <= kQ8Cols ? H : tiles(b, kQ8Cols) * H;
     units16 += n;
-    work16 += n * lens[b];
+    if (units16 <= kQ8Groups) work16 += n * lens[b];
     if (rows > kFewRows) units256 += tiles(b, kQ8PromptCols) * H;
   }
   const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18);

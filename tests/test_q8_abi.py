@@ -186,3 +186,18 @@ def test_rotary_outputs_whose_rows_overlap():
             st = L.okvq_rotary(par, batch, heads, heads, n, ok, ok, FAKE, None, args["qo"], args["ko"], 0, 0, None)
             assert st == -1, (batch, heads, n, bad)
         assert L.okvq_rotary(par, batch, heads, heads, n, ok, ok, FAKE, i32(*[0] * batch), out, out, 0, 0, None) == 0
+
+
+def test_attention_of_absurd_sizes():
+    """Counts that no memory holds are refused, whatever the plan's arithmetic would make of them."""
+    L = q8.lib()
+    top = (1 << 31) - 1
+    for B, H, Hq in ((1, 1, 1), (1, 1, 16), (1, 4096, 65536), (3, 64, 64), (1024, 4096, 65536)):
+        d = dims(batch=B, num_kv_heads=H, num_q_heads=Hq, num_pages=1 << 20, max_pages=(1 << 27) // 64)
+        for rows in (top, 1 << 30, 1 << 28):
+            for n in (1 << 27, 1, 0):
+                if -(-rows * Hq // H // 256) * H * 512 < 1 << 32:
+                    continue  # a launch
+                st = L.okvq_q8_attention(ctypes.byref(cache(d)), 0, i32(*[n] * B), FAKE, i32(*[rows] * B), FAKE, top, ctypes.c_float(0.1), FAKE,
+                                         FAKE, 1 << 40, 0, None)
+                assert st == -2, (B, H, Hq, rows, n)
