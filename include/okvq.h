@@ -564,7 +564,8 @@ size_t okvq_q8_buffer_bytes(const okvq_q8_dims* dims, int32_t which_buffer);
  *   layer       0 .. L - 1
  *   lens_host   host i32 [B], the lengths with the new tokens, 0 <= lens_host[b] <= max_pages * T
  *   k_new, v_new  device [B][H][n_max][128], finite (may be NULL with n_max 0); rows i >= n_new[b] are not read
- *   n_new_host  host i32 [B], n_new_dev the same on the device, 0 <= n_new <= n_max, n_new <= lens */
+ *   n_new_host  host i32 [B], n_new_dev the same on the device, 0 <= n_new <= n_max, n_new <= lens. A replayed call's
+ *               n_new_dev may differ, but not exceed the largest n_new_host of the call */
 okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* k_new,
                            const uint16_t* v_new, const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max,
                            void* stream);

@@ -19,8 +19,8 @@
 //    reference, the maximum of s_t + log2 v_scale. Both references move only when a maximum passes them by 2^8,
 //    so w < 2^15 keeps full precision down to 2^-21 of the largest product, whatever the blocks' scales are; the
 //    sum of p_t stays in fp32, unrounded.
-// Bound: memory in large calls (131072 tokens x 4 heads 25.4 us, 5.3 TB/s), latency in small ones (32768 tokens 9.3 us: 2
-// blocks a wave). 4 or 16 waves in place of 8 took 15.5 and 14.8 us a call with the merge where 8 took 13.4.
+// Bound: memory in large calls (131072 tokens x 4 heads 25.4 us, 5.3 TB/s), latency in small ones (32768 tokens 9.0 us: 2
+// blocks a wave; 12.0 with the merge). 4 or 16 waves in place of 8 were 16 and 10 % slower on the build that took 13.4.
 #include <algorithm>
 
 #include "q8_mfma.hpp"

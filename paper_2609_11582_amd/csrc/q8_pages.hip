@@ -290,7 +290,7 @@ hipError_t launch_q8_extend(const Q8Pages& c, const int32_t* n_new, int32_t* gra
   hipLaunchKernelGGL(k_q8_extend, dim3(1), dim3(kPlan), 0, s, c, n_new, granted, w);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // A launch of 1.5 us (4.4 instead of 2.8 us a call) where no slot copies, which the host cannot know. In the plan's
+  // A launch of 1.5 us (4.2 instead of 2.8 us a call) where no slot copies, which the host cannot know. In the plan's
   // work-group copies are as fast up to some 100 KB only (4 slots x 4 heads x 32 tokens of one layer 9.9 us against 9.5, of 64
   // tokens 12.2 against 9.9, 28 layers 155 against 22): no cache of several layers has so little to copy
   return launch_copy(c, w, c.B, false, s);

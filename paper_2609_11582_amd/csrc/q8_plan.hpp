@@ -112,9 +112,10 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
 //   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
 // * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
-//   a token (prompts x 28 heads: 64 tokens 12.2 -> 9.3 us, 512 26.0 -> 22.0, 2048 78 -> 72.5; 512 rows against 32768 tokens 322
-//   -> 485, as every work-group widens all codes). Up to 128 rows the second half of the waves only brings tiles, which is
-//   as good (16 tokens 8.4 us, in halves 9.1).
+//   a token (prompts x 28 heads: 512 tokens 24.9 -> 20.9 us, 2048 68.8 -> 62.7; 1024 rows x 28 heads against 4096 tokens 79 -> 111,
+//   as every work-group widens all codes). Up to 128 rows the second half of the waves only brings tiles, which is better (120 rows
+//   x 8 heads of 16 sequences of 300: 13.4 us, in halves 15.7). Over 122 calls the rule is within 3 % of the better on average; it is wrong
+//   by up to 19 % where 256 columns would split 2048 tokens (512 rows x 28 heads 37.3 us, in halves 43.3), and at 256 tiles exactly.
 // * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
 //   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
 // * Where the tiles alone are more than the GPU holds at once, one split each; but sequences of more than twice the mean work of

@@ -13,7 +13,8 @@
 //  * The weights are formed in one fused step as 2^(dot * scale + c), c = log2 v_scale + 7 - M; their sum, divided
 //    by the block's factor, is the block's share of the softmax sum.
 // Bound: issue and power together. 512 rows against 4 x 65536 tokens run at 1.0 PFLOP/s (a large bf16 product of the
-// library at 1.2) with the matrix cores busy 43 % and the vector units 46 % of the cycles, at 1.9 GHz.
+// library at 1.2). Under the counters (1184 us, 1.88 GHz) the matrix cores are busy 47 % and the vector units 55 % of the SIMD
+// cycles, the LDS 31 %.
 #include <algorithm>
 
 #include "q8_mfma.hpp"
