@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   Q8Order order = p.splits.order;
   uint32_t w = p.splits.part[q8_part_index(layer)], next = p.splits.part[q8_part_index(layer) + 1];
   __asm__ volatile(""
-                   : "+s"(ntile), "+s"(order.split_slots), "+s"(order.slots), "+s"(order.reordered), "+s"(order.most), "+s"(w), "+s"(next)
+                   : "+s"(ntile), "+s"(order.split_slots), "+s"(order.slots), "+s"(order.flags), "+s"(order.most), "+s"(w), "+s"(next)
                    : "s"(c.k_codes), "s"(c.table), "s"(c.lens), "s"(c.H), "s"(c.max_pages), "s"(p.q), "s"(p.n_new), "s"(p.n_max), "s"(p.G));
   const int h = blockIdx.y / ntile, tile = blockIdx.y - h * ntile;
   const int r0 = tile * kQ8Cols;  // first row of the tile
@@ -54,10 +54,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   if (mine.none) return;
   int b = place;
   const int split = mine.split, nsplit = mine.nsplit;
-  if (order.reordered) {
-    b = q8_slot_at(p.splits, place);
-    if (place >= order.active_slots && uniform_load(p.n_new + b) <= 0) return;  // before it loads anything in advance
-  }
+  if (order.flags & kQ8Reordered) b = q8_slot_at(p.splits, place);
+  // tiles that may have no rows, before they load anything in advance
+  if ((order.flags & kQ8Uneven) && (tile > 0 || place >= order.active_slots) && r0 >= (int64_t)uniform_load(p.n_new + b) * p.G) return;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, col = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* row = c.table + (int64_t)b * c.max_pages;
@@ -248,13 +247,13 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_merge(Q8AttendArgs 
   Q8Order order = p.splits.order;
   uint32_t w = p.splits.part[place], next = p.splits.part[place + 1];
   __asm__ volatile(""  // one wait for them
-                   : "+s"(ntile), "+s"(order.reordered), "+s"(w), "+s"(next)
+                   : "+s"(ntile), "+s"(order.flags), "+s"(w), "+s"(next)
                    : "s"(p.ws), "s"(p.n_new), "s"(p.n_max), "s"(p.G), "s"(p.out), "s"(p.c.H), "s"(cols));
   const int h = blockIdx.y / ntile, tile = blockIdx.y - h * ntile;
   const int tid = threadIdx.x, lane = tid & 31, grp = (tid >> 5) % kGroups, cc = blockIdx.x * kCols + (tid >> 5) / kGroups;
   const Q8Part mine = q8_part(order, w, next, place, 0, tile);
   if (mine.records == 0) return;
-  const int nsplit = mine.nsplit, b = order.reordered ? q8_slot_at(p.splits, place) : place;
+  const int nsplit = mine.nsplit, b = order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
   const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int r = tile * cols + cc, i = r / p.G, hq = h * p.G + (r - i * p.G);
   const bool live = i < n;

@@ -20,13 +20,15 @@ constexpr int kQ8Record = 128 + 4;   // floats of a column's record: its sums, a
 // Launch order of the slots: first those whose sequence is split (a record takes a split, a tile and a head, and there are
 // kQ8Groups at most: 256 slots), then the others with new rows, then those without.
 struct Q8Order {
-  int split_slots, active_slots, slots, reordered;
-  int most;  // splits of the sequence that has most
+  int split_slots, active_slots, slots;
+  int flags;  // kQ8Reordered: places are not the slots themselves; kQ8Uneven: some slot has fewer tiles than the launch
+  int most;   // splits of the sequence that has most
 };
+constexpr int kQ8Reordered = 1, kQ8Uneven = 2;
 struct Q8Splits {
   Q8Order order;
   uint32_t part[kQ8Groups / 2 + 2];  // of each split slot: splits << 16 | records of one head in the slots before it
-  uint32_t slot[kQ8MaxBatch / 2];    // of each place in the order, two 16-bit numbers a dword; read where `reordered`
+  uint32_t slot[kQ8MaxBatch / 2];    // of each place in the order, two 16-bit numbers a dword; read where kQ8Reordered
 };
 struct Q8Plan {
   int cols;    // query columns of a tile: rows of a KV head's group, G to a position
@@ -106,7 +108,9 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 //   the cache, are few: in 390 calls of 113 to 8192 rows within both bounds it takes 0.36 to 0.84 of the prompt kernel's time
 //   (16 positions x 7 heads at 1024 tokens 18.5 -> 9.4 us, a prompt of 100 x 28 heads 11 -> 5.9). With 640 work-groups it
 //   takes up to 1.11, with 1152 1.57 (16 prompts of 40), at 2^18.6 tile tokens 1.16 (4 sequences of 2048, 8 heads, 84 rows), at
-//   2^19.6 1.6 (16 sequences of 8192, 1 head, 84 rows: 38 us against 23.6).
+//   2^19.6 1.6 (16 sequences of 8192, 1 head, 84 rows: 38 us against 23.6). Tiles that only the largest slot has cost the
+//   others a work-group each: up to 8192 of them it is faster all the same (100 rows beside 15 single tokens of 4 heads 14.5 us
+//   against 25.9, 250 rows beside 63 of 1 head 16.7 against 26.0), with 11000 no longer (one prompt of 100 in 64 slots 16.1 against 10.9).
 // * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
 //   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
@@ -127,7 +131,7 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new) {
   const int64_t rows = (int64_t)most_new * G;
   const auto tiles = [&](int b, int cols) { return ((int64_t)n_new[b] * G + cols - 1) / cols; };
-  int longest = 0, active = 0;
+  int longest = 0, active = 0, fewest = most_new;
   int64_t units16 = 0, units256 = 0, work16 = 0;  // tiles of all heads, and tiles x tokens
   for (int b = 0; b < B; ++b) {
     if (n_new[b] == 0) continue;
@@ -136,9 +140,11 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     const int64_t n = rows <= kQ8Cols ? H : tiles(b, kQ8Cols) * H;
     units16 += n;
     if (units16 <= kQ8Groups) work16 += n * lens[b];
+    fewest = std::min(fewest, n_new[b]);
     if (rows > kFewRows) units256 += tiles(b, kQ8PromptCols) * H;
   }
-  const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18);
+  const int64_t launched = (rows + kQ8Cols - 1) / kQ8Cols * H * B;
+  const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18 && launched <= 16 * kQ8Groups);
   const bool half = rows > 128 && longest <= 2048 && units256 <= 256;
   p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
@@ -192,8 +198,9 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     records += n * (uint32_t)tiles(b, p.cols);
   }
   s.part[o.split_slots] = records;
-  o.reordered = active < B || (o.split_slots > 0 && o.split_slots < B);
-  if (!o.reordered) return;
+  o.flags = active < B || (o.split_slots > 0 && o.split_slots < B) ? kQ8Reordered : 0;
+  if (active < B || ((int64_t)fewest * G + p.cols - 1) / p.cols < p.ntile) o.flags |= kQ8Uneven;
+  if (!(o.flags & kQ8Reordered)) return;
   std::fill(s.slot, s.slot + (B + 1) / 2, 0u);
   int at[3] = {0, o.split_slots, active};
   for (int b = 0; b < B; ++b) {

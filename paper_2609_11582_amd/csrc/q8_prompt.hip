@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   Q8Order order = p.splits.order;
   int ntile = p.ntile;
   __asm__ volatile(""  // one wait for the arguments
-                   : "+s"(order.split_slots), "+s"(order.active_slots), "+s"(order.slots), "+s"(order.reordered), "+s"(ntile)
+                   : "+s"(order.split_slots), "+s"(order.active_slots), "+s"(order.slots), "+s"(order.flags), "+s"(ntile)
                    : "s"(c.k_codes), "s"(c.table), "s"(c.lens), "s"(c.max_pages), "s"(p.n_new), "s"(p.n_max), "s"(p.G), "s"(c.H));
   const Q8Tile at = q8_tile(order, c.H, ntile, width, blockIdx.x, blockIdx.y);
   if (at.place < 0) return;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   if (at.place < order.split_slots) mine = q8_part(order, p.splits.part[at.place], p.splits.part[at.place + 1], at.place, blockIdx.y, tile);
   else mine.none = false;
   if (mine.none) return;
-  const int b = order.reordered ? q8_slot_at(p.splits, at.place) : at.place, split = mine.split, nsplit = mine.nsplit;
+  const int b = order.flags & kQ8Reordered ? q8_slot_at(p.splits, at.place) : at.place, split = mine.split, nsplit = mine.nsplit;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int32_t* table = c.table + (int64_t)b * c.max_pages;

@@ -1,6 +1,6 @@
 // Host check of the 8-bit attention's launch plan, with the mapping that its kernels use: over random calls, every slot, tile and
 // split is met by exactly one work-group, records lie apart and inside the workspace, no merge has more splits than
-// its kernel holds, and slots without new rows take nothing from the others. Prints "ok" or the first call that breaks a rule.
+// its kernel holds, and slots without new rows take no splits from the others. Prints "ok" or the first call that breaks a rule.
 #include "q8_plan.hpp"
 
 #include <cmath>
@@ -47,13 +47,15 @@ int main() {
     const auto meet = [&](int place, int x, int h, int tile) {
       const Q8Part w = q8_part(p.splits.order, p.splits.part[q8_part_index(place)], p.splits.part[q8_part_index(place) + 1], place, x, tile);
       if (w.none) return;
-      const int b = p.splits.order.reordered ? q8_slot_at(p.splits, place) : place;
+      const int b = p.splits.order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
       if (b >= B || w.split >= w.nsplit || w.nsplit > p.splits.order.most || h >= H || tile >= p.ntile) fail("range", B, H, G, lens, n_new);
       char& m = met[(((size_t)b * H + h) * p.ntile + tile) * p.splits.order.most + w.split];
       if (m) fail("twice", B, H, G, lens, n_new);
       m = 1;
       nsplit[(size_t)b * p.ntile + tile] = w.nsplit;
       if ((place >= p.splits.order.active_slots) != (n_new[b] == 0)) fail("idle", B, H, G, lens, n_new);
+      const bool needed = (int64_t)tile * p.cols < (int64_t)n_new[b] * G;
+      if (!needed && !(p.splits.order.flags & kQ8Uneven)) fail("even tiles", B, H, G, lens, n_new);
       if ((w.records > 0) != (w.nsplit > 1)) fail("records of one split", B, H, G, lens, n_new);
       if (w.records == 0) return;
       if (place >= p.splits.order.split_slots) fail("no merge", B, H, G, lens, n_new);
@@ -78,14 +80,16 @@ int main() {
         for (int i = 0; i < H * n; ++i)
           if (!met[(((size_t)b * H + i / n) * p.ntile + tile) * p.splits.order.most + i % n]) fail("split missed", B, H, G, lens, n_new);
       }
-    // the same call without the slots that have no rows
+    // the same call without the slots that have no rows: the same splits, where as many work-groups without work (a slot's, or a
+    // tile's that it lacks) leave the kernel the same
     std::vector<int32_t> l2, n2;
     for (int b = 0; b < B; ++b)
       if (n_new[b]) l2.push_back(lens[b]), n2.push_back(n_new[b]);
     Q8Plan q;
     q8_plan(q, (int)l2.size(), H, G, most, l2.data(), n2.data());
-    if (q.cols != p.cols || q.splits.order.most != p.splits.order.most || q.splits.order.split_slots != p.splits.order.split_slots ||
-        std::memcmp(q.splits.part, p.splits.part, 4 * (p.splits.order.split_slots + 1)) != 0)
+    if (q.cols != p.cols && (q.cols != kQ8Cols || (int64_t)q.ntile * H * B <= 16 * kQ8Groups)) fail("idle slots change the kernel", B, H, G, lens, n_new);
+    if (q.cols == p.cols && (q.splits.order.most != p.splits.order.most || q.splits.order.split_slots != p.splits.order.split_slots ||
+        std::memcmp(q.splits.part, p.splits.part, 4 * (p.splits.order.split_slots + 1)) != 0))
       fail("idle slots change the plan", B, H, G, lens, n_new);
   }
   // a long sequence among more short ones than the GPU holds at once

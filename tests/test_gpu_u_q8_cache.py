@@ -941,3 +941,19 @@ def test_many_rows_of_many_heads(kind, fmt, dtype, n):
         worst = max(worst, float((np.abs(got[0, j, pick] - ref) / np.maximum(bound, 1e-30)).max()))
     _say(f"many rows of many heads, {kind} {fmt} {dtype} {n}: worst err / bound {worst:.3f}")
     assert worst <= 1
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("lens, new", [
+    ([300, 500, 40, 0, 500, 2, 300, 7], [250, 1, 1, 0, 17, 2, 1, 0]),       # one split each, the first alone has many tiles
+    ([3000, 2500, 700, 60, 3100, 0, 2900, 4], [40, 1, 3, 1, 2, 0, 0, 4]),  # splits of some
+])
+def test_many_tiles_beside_few(fmt, dtype, lens, new):
+    """The split kernel with a slot of many tiles beside slots of one."""
+    B, n = len(lens), max(new)
+    c = _filled(B, 1, 7, lens, 64, fmt, dtype, 221)
+    q = _rows(222, B, 7, n, 128, dtype=dtype)
+    for b in range(B):
+        q[b, :, new[b]:] = float("nan")
+    out = _attend(c, lens, q, new)
+    _check_attention(c, out, lens, q, new, fmt, dtype, f"many tiles beside few {fmt} {new}", rows=np.array([0, 1, 2, 16, 39, 120, 249]))
