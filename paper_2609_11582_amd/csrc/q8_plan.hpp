@@ -111,17 +111,18 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 //   2^19.6 1.6 (16 sequences of 8192, 1 head, 84 rows: 38 us against 23.6). Tiles that only the largest slot has cost the
 //   others a work-group each: up to 8192 of them it is faster all the same (100 rows beside 15 single tokens of 4 heads 14.5 us
 //   against 25.9, 250 rows beside 63 of 1 head 16.7 against 26.0), with 11000 no longer (one prompt of 100 in 64 slots 16.1 against 10.9).
-// * One split up to 4 rounds of a block for each wave, which saves the merge launch: 512 tokens 9.2 -> 6.4 us, 1024
-//   tokens 9.2 -> 8.9, 1500 tokens 9.2 -> 11.3.
-// * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 13.6 us, with 128 splits 15.6),
-//   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 20.4 -> 16.2 us).
+// * One split up to 4 rounds of a block for each wave, which saves the merge launch (on the device; the host has one launch
+//   less to make too): 300 tokens 8.4 -> 6.2 us, 512 8.5 -> 7.0, 1024 8.6 -> 9.2.
+// * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 11.2 us, with 128 splits 13.1),
+//   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 18.3 -> 14.4 us).
 // * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
 //   a token (prompts x 28 heads: 512 tokens 24.9 -> 20.9 us, 2048 68.8 -> 62.7; 1024 rows x 28 heads against 4096 tokens 79 -> 111,
 //   as every work-group widens all codes). Up to 128 rows the second half of the waves only brings tiles, which is better (120 rows
 //   x 8 heads of 16 sequences of 300: 13.4 us, in halves 15.7). Over 122 calls the rule is within 3 % of the better on average; it is wrong
 //   by up to 19 % where 256 columns would split 2048 tokens (512 rows x 28 heads 37.3 us, in halves 43.3), and at 256 tiles exactly.
-// * A prompt kernel's split has 512 tokens or more, or 256 in sequences where its record weighs less (64 rows x 7 heads
-//   at 8192 tokens 37 -> 33 us; 4 prompts of 300 tokens 20 us, in splits 29).
+// * A prompt kernel's split has 256 tokens or more, or 512 in sequences below 1024, where a record weighs more than a split
+//   saves (512 rows x 28 heads at 512 tokens 20.8 us, in splits of 256 24.4, 4 chunks of 75 at 300 15.8 and 18.8; at 1024 tokens 256
+//   rows x 28 heads 26.3 -> 22.8, 2048 tokens 512 rows x 7 heads 25.6 -> 23.1, 8192 tokens 64 rows x 28 heads 34.3 -> 29.9).
 // * Where the tiles alone are more than the GPU holds at once, one split each; but sequences of more than twice the mean work of
 //   a place are split into such means, as far as there are records (4 heads, one token: 200 sequences of 300 tokens and one of
 //   131072 627 -> 38.5 us, 200 spread over 64 to 16384 176 -> 132). From the mean itself on, 200 of 2000 and one of 4096
@@ -150,7 +151,7 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
   p.rows = (int)std::min<int64_t>(rows, p.cols);
   const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
-  const int64_t round = few ? 256 : longest < 4096 ? 512 : 256;  // tokens of a round
+  const int64_t round = few ? 256 : longest < 1024 ? 512 : 256;  // tokens of a round
   int64_t units = few ? units16 : units256;
   if (half) {
     units = 0;
