@@ -493,6 +493,41 @@ okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t
                         const int32_t* lens_host, const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype,
                         uint32_t flags, void* stream);
 
+/* ---- Head norms with rotary positions -----------------------------------------------------------
+ * Models that norm every head's row of queries and keys before the rotation: a row x of 128 channels becomes
+ *   R (w * x * r),  r = 1 / sqrt(mean(x^2) + eps),
+ * with R the rotation of okvq_rotary, w a weight per channel shared by the heads of a kind. Computed in fp32 (the sum of
+ * squares has to stay inside its range: magnitudes below 2^60), each row rounded once. */
+
+/* Norm and rotate queries and keys in one launch: okvq_rotary's arguments, and
+ *   q_weight, k_weight  device fp32 [128] of each kind that is given, 16-byte aligned
+ *   eps        2^-126 or more, finite
+ *   flags      OKVQ_ROTARY_ADJACENT */
+okvq_status okvq_norm_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                             int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const float* q_weight,
+                             const float* k_weight, float eps, const int32_t* positions, const int32_t* lens_host,
+                             const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype, uint32_t flags, void* stream);
+
+/* Device workspace bytes of okvq_norm_rotary_backward (0 for invalid arguments; 1 MiB whatever the call). No initial
+ * contents; calls that may overlap, captured graphs among them, need one each. */
+size_t okvq_norm_rotary_workspace_bytes(int32_t batch, int32_t n_tokens);
+
+/* Gradients of okvq_norm_rotary, from its inputs and the gradients of its outputs: with g = R^T dy,
+ *   dx = r (w g - x r^2 mean(w g x)),  dw = sum over the rows of g x r.
+ *   q, k, q_weight, k_weight, eps, positions, lens_host, dtype, flags  as in the forward call
+ *   q_grad, k_grad  device rows: gradients of q_out and k_out
+ *   dq, dk     device rows, as the outputs of okvq_rotary; one may be its own gradient or input with the same strides (in
+ *              place) and may not overlap a row that is read otherwise. Rows t >= lens_host[b] are left as they were
+ *   dq_weight, dk_weight  device fp32 [128], overwritten with the sums over all rows (zero where there are none), in an order
+ *              that depends on the sizes alone: the same inputs give the same bits
+ *   workspace  device, 16-byte aligned, okvq_norm_rotary_workspace_bytes(batch, n_tokens) bytes */
+okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                                      int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const float* q_weight,
+                                      const float* k_weight, float eps, const int32_t* positions, const int32_t* lens_host,
+                                      const okvq_rows* q_grad, const okvq_rows* k_grad, const okvq_rows* dq,
+                                      const okvq_rows* dk, float* dq_weight, float* dk_weight, int32_t dtype,
+                                      void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+
 /* ---- Paged 8-bit cache --------------------------------------------------------------------------
  * Keys and values in 8 bits with one scale for each block of 32 tokens and KV head, in pages that
  * sequences share: a nearly lossless cache beside the packed one, for samples of one prompt and

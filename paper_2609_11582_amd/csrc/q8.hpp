@@ -22,6 +22,21 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(const RotaryArgs& a, int dtype, int max_len, hipStream_t s);
 
+// ---- head norms with the rotation ----------------------------------------------------------------
+struct NormRotaryArgs {
+  RotaryArgs r;             // q_out, k_out: the gradients of q and k in the backward pass
+  const float* q_weight;
+  const float* k_weight;
+  float eps;
+  okvq_rows q_grad, k_grad; // backward: gradients of what the forward pass wrote
+  float* parts;             // backward: [n][2][128] sums of work-groups
+};
+constexpr int kNormParts = 1024;  // work-groups of a backward pass at most (four to a compute unit), or its launches
+hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, hipStream_t s);
+int norm_rotary_parts(int max_len, int nb, int launches);  // work-groups of one of the launches of a backward pass
+hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s);
+hipError_t launch_norm_weight_sum(const float* parts, int n, float* dq_weight, float* dk_weight, hipStream_t s);
+
 // ---- 8-bit cache ---------------------------------------------------------------------------------
 // One layer of a cache
 struct Q8View {

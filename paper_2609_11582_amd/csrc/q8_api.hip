@@ -1,4 +1,4 @@
-// C ABI of the rotary positions and the paged 8-bit cache: argument checks and launch planning.
+// C ABI of the rotary positions, the head norms and the paged 8-bit cache: argument checks and launch planning.
 // Declarations and contracts: include/okvq.h.
 #include <algorithm>
 #include <cmath>
@@ -121,6 +121,85 @@ uint64_t turn_fraction(double f) {
   return bits >> 63 ? 0 - t : t;
 }
 
+// The rows of one kind (queries or keys) of a rotation: an input, an output, and in a backward pass a gradient
+struct RotaryRows {
+  const okvq_rows* in;
+  const okvq_rows* out;
+  const okvq_rows* grad = nullptr;
+  bool backward = false;
+};
+
+// Checks a rotation's arguments and fills what its launches share
+okvq_status rotary_args(RotaryArgs& a, const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                        int32_t n_tokens, const RotaryRows& q, const RotaryRows& k, const int32_t* positions,
+                        const int32_t* lens_host, int32_t dtype, uint32_t flags, uint32_t known_flags) {
+  if (!params || batch < 1 || batch > 65535 || n_tokens < 0 || !rows_at(positions, n_tokens)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (flags & ~known_flags) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (dtype != OKVQ_F16 && dtype != OKVQ_BF16) return OKVQ_ERR_INVALID_ARGUMENT;
+  for (const RotaryRows* r : {&q, &k})
+    if (!r->in != !r->out || (r->backward && !r->in != !r->grad)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!q.in && !k.in) return OKVQ_ERR_INVALID_ARGUMENT;
+  if ((q.in && q_heads < 1) || (k.in && kv_heads < 1)) return OKVQ_ERR_INVALID_ARGUMENT;
+  const int hq = q.in ? q_heads : 0, hk = k.in ? kv_heads : 0;
+  if ((int64_t)hq + hk > 65535) return OKVQ_ERR_UNSUPPORTED;
+  for (const okvq_rows* r : {q.in, k.in, q.out, k.out, q.grad, k.grad})
+    if (r && check_rows_of(r, n_tokens) != OKVQ_OK) return OKVQ_ERR_INVALID_ARGUMENT;
+  a.q = a.k = a.q_out = a.k_out = okvq_rows{};
+  for (int i = 0; i < 64; ++i) {
+    if (params->axis[i] > 2 || !std::isfinite(params->inv_freq[i])) return OKVQ_ERR_INVALID_ARGUMENT;
+    a.axis[i] = params->axis[i];
+    a.turn[i] = turn_fraction(params->inv_freq[i]);
+  }
+  if (q.in) {
+    a.q = *q.in;
+    a.q_out = *q.out;
+  }
+  if (k.in) {
+    a.k = *k.in;
+    a.k_out = *k.out;
+  }
+  a.pos = positions;
+  a.hq = hq;
+  a.hk = hk;
+  a.n = n_tokens;
+  a.flags = flags;
+  int longest = lens_host ? 0 : n_tokens;
+  if (lens_host)
+    for (int b = 0; b < batch; ++b) {
+      if (lens_host[b] < 0 || lens_host[b] > n_tokens) return OKVQ_ERR_INVALID_ARGUMENT;
+      longest = std::max(longest, lens_host[b]);
+    }
+  if (longest > 0 && ((q.in && !rows_apart(*q.out, batch, hq, longest)) || (k.in && !rows_apart(*k.out, batch, hk, longest))))
+    return OKVQ_ERR_INVALID_ARGUMENT;
+  return OKVQ_OK;
+}
+
+// Launches of 256 sequences each; launch: of the rows of the longest one
+template <typename Launch>
+okvq_status rotary_launches(RotaryArgs& a, int32_t batch, const int32_t* lens_host, Launch&& launch) {
+  for (int b0 = 0; b0 < batch; b0 += kMaxLenArgs) {
+    a.b0 = b0;
+    a.nb = std::min(kMaxLenArgs, batch - b0);
+    int most = 0;
+    for (int i = 0; i < a.nb; ++i) {
+      a.lens.lens[i] = lens_host ? lens_host[b0 + i] : a.n;
+      most = std::max(most, a.lens.lens[i]);
+    }
+    const okvq_status st = hip_status(launch(most));
+    if (st != OKVQ_OK) return st;
+  }
+  return OKVQ_OK;
+}
+
+okvq_status norm_args(NormRotaryArgs& a, const float* q_weight, const float* k_weight, float eps) {
+  if ((a.r.hq && !aligned16(q_weight)) || (a.r.hk && !aligned16(k_weight))) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!(eps >= 0x1p-126f) || !std::isfinite(eps)) return OKVQ_ERR_INVALID_ARGUMENT;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.eps = eps;
+  return OKVQ_OK;
+}
+
 // distinct slots of B; `seen` marks them (arrays on the stack: nothing here throws)
 okvq_status check_slots(const int32_t* slots, int n, int B, bool (&seen)[kQ8MaxBatch]) {
   for (int i = 0; i < n; ++i) {
@@ -143,55 +222,57 @@ extern "C" {
 okvq_status okvq_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t n_tokens,
                         const okvq_rows* q, const okvq_rows* k, const int32_t* positions, const int32_t* lens_host,
                         const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype, uint32_t flags, void* stream) {
-  if (!params || batch < 1 || batch > 65535 || n_tokens < 0 || !rows_at(positions, n_tokens)) return OKVQ_ERR_INVALID_ARGUMENT;
-  if (flags & ~(uint32_t)(OKVQ_ROTARY_INVERSE | OKVQ_ROTARY_ADJACENT)) return OKVQ_ERR_INVALID_ARGUMENT;
-  if (dtype != OKVQ_F16 && dtype != OKVQ_BF16) return OKVQ_ERR_INVALID_ARGUMENT;
-  if (!q != !q_out || !k != !k_out || (!q && !k)) return OKVQ_ERR_INVALID_ARGUMENT;
-  if ((q && q_heads < 1) || (k && kv_heads < 1)) return OKVQ_ERR_INVALID_ARGUMENT;
-  const int hq = q ? q_heads : 0, hk = k ? kv_heads : 0;
-  if ((int64_t)hq + hk > 65535) return OKVQ_ERR_UNSUPPORTED;
-  for (const okvq_rows* r : {q, k, q_out, k_out})
-    if (r && check_rows_of(r, n_tokens) != OKVQ_OK) return OKVQ_ERR_INVALID_ARGUMENT;
   RotaryArgs a;
-  a.q = a.k = a.q_out = a.k_out = okvq_rows{};
-  for (int i = 0; i < 64; ++i) {
-    if (params->axis[i] > 2 || !std::isfinite(params->inv_freq[i])) return OKVQ_ERR_INVALID_ARGUMENT;
-    a.axis[i] = params->axis[i];
-    a.turn[i] = turn_fraction(params->inv_freq[i]);
-  }
-  if (q) {
-    a.q = *q;
-    a.q_out = *q_out;
-  }
-  if (k) {
-    a.k = *k;
-    a.k_out = *k_out;
-  }
-  a.pos = positions;
-  a.hq = hq;
-  a.hk = hk;
-  a.n = n_tokens;
-  a.flags = flags;
-  int longest = lens_host ? 0 : n_tokens;
-  if (lens_host)
-    for (int b = 0; b < batch; ++b) {
-      if (lens_host[b] < 0 || lens_host[b] > n_tokens) return OKVQ_ERR_INVALID_ARGUMENT;
-      longest = std::max(longest, lens_host[b]);
-    }
-  if (longest > 0 && ((q && !rows_apart(*q_out, batch, hq, longest)) || (k && !rows_apart(*k_out, batch, hk, longest))))
-    return OKVQ_ERR_INVALID_ARGUMENT;
-  for (int b0 = 0; b0 < batch; b0 += kMaxLenArgs) {
-    a.b0 = b0;
-    a.nb = std::min(kMaxLenArgs, batch - b0);
-    int most = 0;
-    for (int i = 0; i < a.nb; ++i) {
-      a.lens.lens[i] = lens_host ? lens_host[b0 + i] : n_tokens;
-      most = std::max(most, a.lens.lens[i]);
-    }
-    const okvq_status st = hip_status(launch_rotary(a, dtype, most, static_cast<hipStream_t>(stream)));
-    if (st != OKVQ_OK) return st;
-  }
-  return OKVQ_OK;
+  const okvq_status st = rotary_args(a, params, batch, q_heads, kv_heads, n_tokens, {q, q_out}, {k, k_out}, positions, lens_host,
+                                     dtype, flags, OKVQ_ROTARY_INVERSE | OKVQ_ROTARY_ADJACENT);
+  if (st != OKVQ_OK) return st;
+  return rotary_launches(a, batch, lens_host, [&](int most) { return launch_rotary(a, dtype, most, static_cast<hipStream_t>(stream)); });
+}
+
+okvq_status okvq_norm_rotary(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t n_tokens,
+                             const okvq_rows* q, const okvq_rows* k, const float* q_weight, const float* k_weight, float eps,
+                             const int32_t* positions, const int32_t* lens_host, const okvq_rows* q_out, const okvq_rows* k_out,
+                             int32_t dtype, uint32_t flags, void* stream) {
+  NormRotaryArgs a;
+  okvq_status st = rotary_args(a.r, params, batch, q_heads, kv_heads, n_tokens, {q, q_out}, {k, k_out}, positions, lens_host, dtype,
+                               flags, OKVQ_ROTARY_ADJACENT);
+  if (st == OKVQ_OK) st = norm_args(a, q_weight, k_weight, eps);
+  if (st != OKVQ_OK) return st;
+  return rotary_launches(a.r, batch, lens_host,
+                         [&](int most) { return launch_norm_rotary(a, dtype, most, static_cast<hipStream_t>(stream)); });
+}
+
+size_t okvq_norm_rotary_workspace_bytes(int32_t batch, int32_t n_tokens) {
+  if (batch < 1 || batch > 65535 || n_tokens < 0) return 0;
+  return (size_t)kNormParts * 2 * kD * sizeof(float);
+}
+
+okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
+                                      int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const float* q_weight,
+                                      const float* k_weight, float eps, const int32_t* positions, const int32_t* lens_host,
+                                      const okvq_rows* q_grad, const okvq_rows* k_grad, const okvq_rows* dq, const okvq_rows* dk,
+                                      float* dq_weight, float* dk_weight, int32_t dtype, void* workspace, size_t workspace_bytes,
+                                      uint32_t flags, void* stream) {
+  NormRotaryArgs a;
+  okvq_status st = rotary_args(a.r, params, batch, q_heads, kv_heads, n_tokens, {q, dq, q_grad, true}, {k, dk, k_grad, true}, positions,
+                               lens_host, dtype, flags, OKVQ_ROTARY_ADJACENT);
+  if (st == OKVQ_OK) st = norm_args(a, q_weight, k_weight, eps);
+  if (st != OKVQ_OK) return st;
+  if ((q && !aligned16(dq_weight)) || (k && !aligned16(dk_weight))) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!aligned16(workspace) || workspace_bytes < okvq_norm_rotary_workspace_bytes(batch, n_tokens)) return OKVQ_ERR_WORKSPACE;
+  a.q_grad = q ? *q_grad : okvq_rows{};
+  a.k_grad = k ? *k_grad : okvq_rows{};
+  a.parts = static_cast<float*>(workspace);
+  const int launches = (batch + kMaxLenArgs - 1) / kMaxLenArgs;
+  int parts = 0;
+  st = rotary_launches(a.r, batch, lens_host, [&](int most) {
+    const int groups = norm_rotary_parts(most, a.r.nb, launches), part0 = parts;
+    parts += groups;
+    return launch_norm_rotary_grad(a, dtype, most, part0, groups, static_cast<hipStream_t>(stream));
+  });
+  if (st != OKVQ_OK) return st;
+  return hip_status(launch_norm_weight_sum(a.parts, parts, q ? dq_weight : nullptr, k ? dk_weight : nullptr,
+                                           static_cast<hipStream_t>(stream)));
 }
 
 size_t okvq_q8_buffer_bytes(const okvq_q8_dims* d, int32_t which) {

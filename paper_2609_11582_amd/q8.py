@@ -54,10 +54,15 @@ def lib() -> ctypes.CDLL:
     global _ready
     if _ready is None:
         L = _okvq_lib()
-        vp, i32, u32, sz, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t, ctypes.POINTER
+        vp, i32, u32, sz, f32, P = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_size_t, ctypes.c_float,
+                                   ctypes.POINTER)
         for name, res, args in (
                 # okvq_rows as packed bytes (_rows_of) or Rows structures, host counts as packed bytes (_ints) or arrays
                 ("okvq_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, u32, vp]),
+                ("okvq_norm_rotary", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp, i32, u32, vp]),
+                ("okvq_norm_rotary_workspace_bytes", sz, [i32, i32]),
+                ("okvq_norm_rotary_backward", i32, [P(RotaryParams), i32, i32, i32, i32, vp, vp, vp, vp, f32, vp, vp, vp, vp, vp, vp,
+                                                    vp, vp, i32, vp, sz, u32, vp]),
                 ("okvq_q8_buffer_bytes", sz, [P(Q8Dims), i32]),
                 ("okvq_q8_append", i32, [P(Q8Struct), i32, vp, vp, vp, vp, vp, i32, vp]),
                 ("okvq_q8_workspace_bytes", sz, [P(Q8Dims), i32, i32]),
@@ -187,6 +192,85 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
                            oq, ok, _ROW_TYPES[dt], _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_rotary")
+    return st
+
+
+# ---- head norms with the rotation ------------------------------------------------------------------
+
+
+def _norm_rows(q, k, q_more, k_more, names):
+    """Sizes of a call, and the rows of each kind as packed bytes: the input's, then those of q_more or k_more (tensors of the
+    input's shape and type, named by `names`)."""
+    some = q if q is not None else k
+    if (not isinstance(some, torch.Tensor) or not some.is_cuda or some.dim() != 4 or some.dtype not in _ROW_TYPES
+            or some.shape[3] != 128):
+        raise ValueError("q, k: expected fp16 or bf16 device tensors [batch][heads][tokens][128]")
+    B, _, n, _ = some.shape
+    dt, device = some.dtype, _device()
+    heads, rows = [], []
+    for kind, x, more in (("q", q, q_more), ("k", k, k_more)):
+        if any((x is None) != (y is None) for y in more):
+            raise ValueError(f"{kind}: the rows and all that belongs to them, or none of it")
+        if x is None:
+            heads.append(0)
+            rows.append((None,) * (1 + len(more)))
+            continue
+        h = x.shape[1] if isinstance(x, torch.Tensor) and x.dim() == 4 else 0
+        shape = (B, h, n, 128)
+        heads.append(h)
+        rows.append(tuple(_rows_of(y, shape, dt, name.format(kind), device) for y, name in zip((x, *more), ("{}",) + names)))
+    return B, heads, n, dt, device, rows
+
+
+def _norm_weight(w, x, name: str, device: int):
+    if (w is None) != (x is None):
+        raise ValueError(f"{name}: one for each kind of rows that is given")
+    return None if w is None else _need_rows(w, (128,), torch.float32, name, device)
+
+
+def _positions_of(positions, B, n, device):
+    pos = _need(positions, 0, torch.int32, "positions", device)
+    if positions.shape != (B, 3, n):
+        raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
+    return pos
+
+
+def okvq_norm_rotary(rotary: RotaryParams, q, k, q_weight, k_weight, eps, positions, q_out, k_out, lens=None, flags=0, stream=None,
+                     check=True) -> int:
+    """okvq_rotary of rows divided by their root mean square (of the 128 channels, with eps) and weighted: q_weight,
+    k_weight fp32 [128], or None with their rows."""
+    B, (hq, hk), n, dt, device, ((rq, oq), (rk, ok)) = _norm_rows(q, k, (q_out,), (k_out,), ("{}_out",))
+    st = lib().okvq_norm_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, _norm_weight(q_weight, q, "q_weight", device),
+                                _norm_weight(k_weight, k, "k_weight", device), float(eps), _positions_of(positions, B, n, device),
+                                None if lens is None else _ints(lens, B, "lens"), oq, ok, _ROW_TYPES[dt],
+                                _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
+    if check and st:
+        _check(st, "okvq_norm_rotary")
+    return st
+
+
+def okvq_norm_rotary_workspace_bytes(batch: int, n_tokens: int) -> int:
+    return lib().okvq_norm_rotary_workspace_bytes(_int(batch, "batch"), _int(n_tokens, "n_tokens"))
+
+
+def norm_rotary_workspace(batch: int, n_tokens: int, device="cuda") -> torch.Tensor:
+    """A workspace of okvq_norm_rotary_workspace_bytes bytes for okvq_norm_rotary_backward (no contents needed)."""
+    return torch.empty(max(okvq_norm_rotary_workspace_bytes(batch, n_tokens) + 15, 16) // 16 * 4, dtype=torch.float32, device=device)
+
+
+def okvq_norm_rotary_backward(rotary: RotaryParams, q, k, q_weight, k_weight, eps, positions, q_grad, k_grad, dq, dk, dq_weight,
+                              dk_weight, workspace, lens=None, flags=0, stream=None, check=True) -> int:
+    """Gradients of okvq_norm_rotary: q_grad, k_grad of its outputs; dq, dk (rows, any strides) and dq_weight, dk_weight
+    (fp32 [128], overwritten) are written."""
+    B, (hq, hk), n, dt, device, ((rq, gq, oq), (rk, gk, ok)) = _norm_rows(q, k, (q_grad, dq), (k_grad, dk), ("{}_grad", "d{}"))
+    st = lib().okvq_norm_rotary_backward(
+        ctypes.byref(rotary), B, hq, hk, n, rq, rk, _norm_weight(q_weight, q, "q_weight", device),
+        _norm_weight(k_weight, k, "k_weight", device), float(eps), _positions_of(positions, B, n, device),
+        None if lens is None else _ints(lens, B, "lens"), gq, gk, oq, ok, _norm_weight(dq_weight, q, "dq_weight", device),
+        _norm_weight(dk_weight, k, "dk_weight", device), _ROW_TYPES[dt], _need(workspace, 0, None, "workspace", device),
+        workspace.nbytes, _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
+    if check and st:
+        _check(st, "okvq_norm_rotary_backward")
     return st
 
 
