@@ -631,6 +631,48 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
                               const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, float sm_scale,
                               uint16_t* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
 
+/* Attention of new rows with a sliding window, for layers whose rows see the newest tokens only: with p = seq_lens[b] -
+ * n_new[b] + i the place of row i, it sees the tokens t <= p with t > p - window or t < sinks (the first tokens stay
+ * visible). Reads those blocks of the cache alone. One token a sequence, a chunk or a whole prompt; the arguments and the
+ * workspace are those of okvq_q8_attention (okvq_q8_workspace_bytes), and
+ *   window      1 or more: tokens that a row sees, its own among them
+ *   sinks       0 or more */
+okvq_status okvq_q8_window_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                                     const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, int32_t window,
+                                     int32_t sinks, float sm_scale, uint16_t* out, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* drafts of a slot in one call at most */
+enum { OKVQ_Q8_MAX_DRAFTS = 256 };
+
+/* Device workspace bytes that okvq_q8_tree_attention needs for up to n_max drafts (0 for invalid arguments): records of 528
+ * bytes for every row of a query head, and those of okvq_q8_workspace_bytes. Enough for fewer drafts too. No initial
+ * contents; calls that may overlap, captured graphs among them, need one each. */
+size_t okvq_q8_tree_workspace_bytes(const okvq_q8_dims* dims, int32_t n_max);
+
+/* Attention of drafted tokens over one layer: a tree of continuations that is verified in one call. Drafts are not in the
+ * cache (a block that took rejected tokens could not give them back): their keys and values come as rows, are attended as
+ * they are, and what is accepted is then appended (okvq_q8_extend, okvq_q8_append).
+ *   lens_host   host i32 [B]: tokens in the cache, without drafts (plans the launch; the kernels read seq_lens)
+ *   q           device [B][Hq][n_max][128], finite: the drafts' queries
+ *   k_draft, v_draft  device [B][H][n_max][128], finite; rows that no mask names are not read
+ *   visible     device u32 [B][n_max][ceil(n_max / 32)]: bit j % 32 of word j / 32 of row i says that row i sees draft j: its
+ *               ancestors and itself. Any masks may be given; bits from n_draft[b] on count as zero
+ *   n_draft_host, n_draft_dev  drafts of each slot, 0 <= n_draft <= n_max <= OKVQ_Q8_MAX_DRAFTS. Where the device has more
+ *               drafts of a slot than the host, those up to the largest n_draft_host of the call are attended all the same
+ *   window      0: a row sees the whole cache. Otherwise it sees, with a the number of drafts that its mask names, the
+ *               tokens t < sinks and those with t > seq_lens[b] + a - 1 - window: what okvq_q8_window_attention would let it
+ *               see once its line were appended, where its mask names window drafts at most
+ *   sinks       0 or more; counts with a window only
+ *   sm_scale, q, out  as in okvq_q8_attention; out rows i >= n_draft[b] are left as they were
+ *   workspace   device, 16-byte aligned, okvq_q8_tree_workspace_bytes(dims, n_max) bytes
+ * A row that sees nothing yields zeros. The cache's part is computed as in okvq_q8_attention, the drafts' part in fp32. */
+okvq_status okvq_q8_tree_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                                   const uint16_t* k_draft, const uint16_t* v_draft, const uint32_t* visible,
+                                   const int32_t* n_draft_host, const int32_t* n_draft_dev, int32_t n_max, int32_t window,
+                                   int32_t sinks, float sm_scale, uint16_t* out, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
 /* Device workspace bytes of okvq_q8_extend and okvq_q8_compact (0 for invalid dims). No initial contents; calls that
  * may overlap (on different caches) need one each. */
 size_t okvq_q8_page_workspace_bytes(const okvq_q8_dims* dims);

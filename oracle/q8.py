@@ -114,6 +114,31 @@ def attention(q, k, v, seen, sm_scale, half_step):
     return out, bound
 
 
+def attention_where(q, k, v, seen, sm_scale, half_step):
+    """attention() of rows that see any tokens: seen [rows][n] truth values. A row that sees none yields zeros."""
+    out, bound = np.zeros((len(q), D)), np.zeros((len(q), D))
+    for r, mask in enumerate(seen):
+        if mask.any():
+            o, e = attention(q[r:r + 1], k[mask], v[mask], [int(mask.sum())], sm_scale, half_step)
+            out[r], bound[r] = o[0], e[0]
+    return out, bound
+
+
+def window_seen(length, n_new, window, sinks):
+    """[n_new][length]: what the newest rows see of a sequence with a window and sinks."""
+    p, t = (length - n_new + np.arange(n_new))[:, None], np.arange(length)
+    return (t <= p) & ((t > p - window) | (t < sinks))
+
+
+def tree_seen(length, visible, n, window, sinks):
+    """[n][length + n]: what drafts see of the cache and of each other; visible u32 [>= n][words], window 0 for none."""
+    j = np.arange(n)
+    named = (visible[:n, j // 32] >> (j % 32).astype(np.uint32) & 1).astype(bool)
+    p, t = (length + named.sum(1) - 1)[:, None], np.arange(length)
+    cached = (t > p - window) | (t < sinks) if window else np.ones((n, length), bool)
+    return np.concatenate([cached, named], 1)
+
+
 class PagedModel:
     """Tables, lengths and holders of a cache under the page calls, one slot after the other, with the page copies
     that they make in `moves` (from, to)."""

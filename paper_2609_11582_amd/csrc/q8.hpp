@@ -70,9 +70,21 @@ struct Q8AttendArgs {
   int n_max, G, ntile, cross;
   float qscale;  // sm_scale log2(e)
   Q8Splits splits;
+  // a window or a tree: a row sees the sinks and the newest `window` tokens up to its own place
+  int window, sinks;
+  // a tree: drafts [B][H][n_max][128], masks [B][n_max][words], and records in front of those of tiles with one split
+  const uint16_t* kd;
+  const uint16_t* vd;
+  const uint32_t* visible;
+  int words;
+  int64_t single;
 };
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s);
-hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s);
+// What a row sees of the cache (template argument of the attention kernels): the tokens up to its own, or all with `cross`;
+// of these the sinks and a window; or what precedes a tree of drafts (all, or sinks and window), whose part a merge adds
+constexpr int kQ8Full = 0, kQ8Window = 1, kQ8Tree = 2;
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s);
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s);
+hipError_t launch_q8_tree_merge(const Q8AttendArgs& a, const Q8Plan& p, int dtype, hipStream_t s);
 
 // Page calls, on the whole cache
 struct Q8Pages {

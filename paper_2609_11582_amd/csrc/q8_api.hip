@@ -200,6 +200,55 @@ okvq_status norm_args(NormRotaryArgs& a, const float* q_weight, const float* k_w
   return OKVQ_OK;
 }
 
+// The refusal of a call whose own arguments are wrong: what is wrong with the cache comes first
+okvq_status cache_or_argument_error(const okvq_q8_cache* c) {
+  const okvq_status st = check_cache(c);
+  return st != OKVQ_OK ? st : OKVQ_ERR_INVALID_ARGUMENT;
+}
+
+// An attention call over a cache: checks, plan, launches; a: what belongs to the span alone (kQ8Full, kQ8Window or kQ8Tree)
+okvq_status attend(Q8AttendArgs& a, int span, const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                   const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, float sm_scale, uint16_t* out,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  okvq_status st = check_cache(cache);
+  if (st != OKVQ_OK) return st;
+  const okvq_q8_dims& d = cache->dims;
+  const float qscale = sm_scale * 1.4426950408889634f;  // log2(e): the kernels' exponentials have base 2
+  if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0 || !std::isfinite(qscale)) return OKVQ_ERR_INVALID_ARGUMENT;
+  if (!rows_at(q, n_max) || !aligned16(n_new_dev) || !rows_at(out, n_max)) return OKVQ_ERR_INVALID_ARGUMENT;
+  int most;
+  st = check_rows(d, lens_host, n_new_host, n_max, true, &most);
+  if (st != OKVQ_OK) return st;
+  if (most == 0) return OKVQ_OK;
+  const int G = d.num_q_heads / d.num_kv_heads;
+  // before the plan, whose products stay inside 64 bits for what can be launched
+  if (!launchable(((int64_t)most * G + kQ8PromptCols - 1) / kQ8PromptCols * d.num_kv_heads, 512)) return OKVQ_ERR_UNSUPPORTED;
+  int32_t spans[kQ8MaxBatch];
+  if (span != kQ8Full) {
+    a.sinks = std::min(a.sinks, capacity(d));
+    for (int b = 0; b < d.batch; ++b) spans[b] = q8_span(lens_host[b], n_new_host[b], G, a.window, a.sinks);
+  }
+  Q8Plan plan;
+  q8_plan(plan, d.batch, d.num_kv_heads, G, most, span == kQ8Full ? lens_host : spans, n_new_host);
+  const size_t need = span == kQ8Tree ? q8_tree_workspace(plan, d.num_kv_heads) : q8_workspace_bound(G, most);
+  if (!aligned16(workspace) || workspace_bytes < need) return OKVQ_ERR_WORKSPACE;
+  const int64_t units = (int64_t)plan.ntile * d.num_kv_heads;
+  if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
+      (plan.splits.order.most > 1 && (!launchable(units * plan.splits.order.split_slots * 32, 256) || units > 65535)) ||
+      (span == kQ8Tree && (!launchable(units * d.batch * plan.rows, 512) || units > 65535)))
+    return OKVQ_ERR_UNSUPPORTED;
+  a.c = view(cache, layer);
+  a.q = q;
+  a.n_new = n_new_dev;
+  a.out = out;
+  a.ws = static_cast<float*>(workspace);
+  a.n_max = n_max;
+  a.G = G;
+  a.qscale = qscale;
+  a.single = q8_split_records(plan, d.num_kv_heads);
+  return hip_status(launch_q8_attention(a, plan, span, d.format, d.dtype, static_cast<hipStream_t>(stream)));
+}
+
 // distinct slots of B; `seen` marks them (arrays on the stack: nothing here throws)
 okvq_status check_slots(const int32_t* slots, int n, int B, bool (&seen)[kQ8MaxBatch]) {
   for (int i = 0; i < n; ++i) {
@@ -320,39 +369,44 @@ size_t okvq_q8_workspace_bytes(const okvq_q8_dims* d, int32_t max_seq_len, int32
 okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
                               const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, float sm_scale,
                               uint16_t* out, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream) {
-  okvq_status st = check_cache(cache);
-  if (st != OKVQ_OK) return st;
-  const okvq_q8_dims& d = cache->dims;
-  const float qscale = sm_scale * 1.4426950408889634f;  // log2(e): the kernels' exponentials have base 2
-  if (layer < 0 || layer >= d.layers || !lens_host || !n_new_host || n_max < 0 || !std::isfinite(qscale) ||
-      (flags & ~(uint32_t)OKVQ_Q8_CROSS))
-    return OKVQ_ERR_INVALID_ARGUMENT;
-  if (!rows_at(q, n_max) || !aligned16(n_new_dev) || !rows_at(out, n_max)) return OKVQ_ERR_INVALID_ARGUMENT;
-  int most;
-  st = check_rows(d, lens_host, n_new_host, n_max, true, &most);
-  if (st != OKVQ_OK) return st;
-  if (most == 0) return OKVQ_OK;
-  const int G = d.num_q_heads / d.num_kv_heads;
-  // before the plan, whose products stay inside 64 bits for what can be launched
-  if (!launchable(((int64_t)most * G + kQ8PromptCols - 1) / kQ8PromptCols * d.num_kv_heads, 512)) return OKVQ_ERR_UNSUPPORTED;
-  Q8Plan plan;
-  q8_plan(plan, d.batch, d.num_kv_heads, G, most, lens_host, n_new_host);
-  if (!aligned16(workspace) || workspace_bytes < q8_workspace_bound(G, most)) return OKVQ_ERR_WORKSPACE;
-  const int64_t units = (int64_t)plan.ntile * d.num_kv_heads;
-  if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
-      (plan.splits.order.most > 1 && (!launchable(units * plan.splits.order.split_slots * 32, 256) || units > 65535)))
-    return OKVQ_ERR_UNSUPPORTED;
-  Q8AttendArgs a;
-  a.c = view(cache, layer);
-  a.q = q;
-  a.n_new = n_new_dev;
-  a.out = out;
-  a.ws = static_cast<float*>(workspace);
-  a.n_max = n_max;
-  a.G = G;
+  if (flags & ~(uint32_t)OKVQ_Q8_CROSS) return cache_or_argument_error(cache);
+  Q8AttendArgs a{};
   a.cross = (flags & OKVQ_Q8_CROSS) ? 1 : 0;
-  a.qscale = qscale;
-  return hip_status(launch_q8_attention(a, plan, d.format, d.dtype, static_cast<hipStream_t>(stream)));
+  return attend(a, kQ8Full, cache, layer, lens_host, q, n_new_host, n_new_dev, n_max, sm_scale, out, workspace, workspace_bytes, stream);
+}
+
+okvq_status okvq_q8_window_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                                     const int32_t* n_new_host, const int32_t* n_new_dev, int32_t n_max, int32_t window,
+                                     int32_t sinks, float sm_scale, uint16_t* out, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  if (window < 1 || sinks < 0) return cache_or_argument_error(cache);
+  Q8AttendArgs a{};
+  a.window = window;
+  a.sinks = sinks;
+  return attend(a, kQ8Window, cache, layer, lens_host, q, n_new_host, n_new_dev, n_max, sm_scale, out, workspace, workspace_bytes, stream);
+}
+
+size_t okvq_q8_tree_workspace_bytes(const okvq_q8_dims* d, int32_t n_max) {
+  if (check_dims(d) != OKVQ_OK || n_max < 1 || n_max > OKVQ_Q8_MAX_DRAFTS) return 0;
+  return q8_tree_workspace_bound(d->batch, d->num_kv_heads, d->num_q_heads / d->num_kv_heads, n_max);
+}
+
+okvq_status okvq_q8_tree_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
+                                   const uint16_t* k_draft, const uint16_t* v_draft, const uint32_t* visible,
+                                   const int32_t* n_draft_host, const int32_t* n_draft_dev, int32_t n_max, int32_t window,
+                                   int32_t sinks, float sm_scale, uint16_t* out, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+  if (window < 0 || sinks < 0 || n_max < 0 || n_max > OKVQ_Q8_MAX_DRAFTS || !rows_at(k_draft, n_max) || !rows_at(v_draft, n_max) ||
+      !rows_at(visible, n_max))
+    return cache_or_argument_error(cache);
+  Q8AttendArgs a{};
+  a.window = window > 0 ? window : INT32_MAX;
+  a.sinks = sinks;
+  a.kd = k_draft;
+  a.vd = v_draft;
+  a.visible = visible;
+  a.words = (n_max + 31) / 32;
+  return attend(a, kQ8Tree, cache, layer, lens_host, q, n_draft_host, n_draft_dev, n_max, sm_scale, out, workspace, workspace_bytes, stream);
 }
 
 size_t okvq_q8_page_workspace_bytes(const okvq_q8_dims* d) {

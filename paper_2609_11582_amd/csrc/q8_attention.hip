@@ -34,7 +34,7 @@ constexpr int kRecFloatsQ8 = kQ8Cols * kQ8Record;  // a split's record: [16][128
 static_assert(kQ8Record == kD + 4 && kWaves * kW == 256, "as the plan counts");
 constexpr int kCombineRow = kD + 4;               // floats of a combine row: 16 rows of a column fall into all banks
 
-template <int kFmt, bool kBf16>
+template <int kSpan, int kFmt, bool kBf16>
 __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
   __shared__ __attribute__((aligned(16))) float cmb[kWaves][kQ8Cols * kCombineRow];
   __shared__ float wM[kWaves][kQ8Cols], wm[kWaves][kQ8Cols], wl[kWaves][kQ8Cols];
@@ -92,20 +92,37 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
     for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint4*>(at + (vo + j * 1024));
     vs = uniform_load(c.v_scale + slot);
   };
-  int64_t slot = q8_slot(q8_page(row, block, c), h, block, c);
-  load_keys(slot);
-  load_values(slot);
-  int page = q8_page(row, block + stride, c);  // of the wave's next block
-  __asm__ volatile("" ::: "memory");           // the loads above go out before the length is waited for
+  int64_t slot;
+  int page;
+  if constexpr (kSpan == kQ8Full) {
+    slot = q8_slot(q8_page(row, block, c), h, block, c);
+    load_keys(slot);
+    load_values(slot);
+    page = q8_page(row, block + stride, c);  // of the wave's next block
+    __asm__ volatile("" ::: "memory");       // the loads above go out before the length is waited for
+  }
 
   const int len = q8_len(c, b), n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int i_first = r0 / p.G, i_last = min((r0 + kQ8Cols - 1) / p.G, n - 1);
   if (i_first >= n) return;
-  const int vis_first = p.cross ? len : max(len - n + i_first + 1, 0);  // tokens that the first and the last row see
-  const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
+  auto cross = [&] { return kSpan == kQ8Tree || (kSpan == kQ8Full && p.cross); };
+  const int vis_first = cross() ? len : max(len - n + i_first + 1, 0);  // tokens that the first and the last row see
+  const int vis_last = cross() ? len : max(len - n + i_last + 1, 0);
   const bool live = i < n;
-  const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
+  const int vis = live ? (cross() ? len : max(len - n + i + 1, 0)) : 0;
   const int nblk = (vis_last + kW - 1) / kW;
+  // with a window the wave's blocks are numbered over those that some row of the tile sees, which the length says
+  const Q8Walk walk(kSpan == kQ8Full ? 0 : p.sinks, q8_from_least<kSpan>(p, len, n, i_first), vis_last, kW);
+  const int from_most = q8_from_most<kSpan>(p, len, n, i_last), end = kSpan == kQ8Full ? nblk : walk.count;
+  auto real = [&](int v) { return kSpan == kQ8Full ? v : walk(v); };
+  int from = 0;
+  if constexpr (kSpan != kQ8Full) {
+    slot = q8_slot(q8_page(row, real(block), c), h, real(block), c);
+    load_keys(slot);
+    load_values(slot);
+    page = q8_page(row, real(block + stride), c);
+    from = live ? q8_sight<kSpan>(p, b, len, n, i).from : 0;
+  }
 
   half8 qop[4];
   float qs = p.qscale;
@@ -119,9 +136,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
 #pragma unroll
   for (int t = 0; t < 8; ++t) acc[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  while (block < nblk) {
-    const int t0 = block * kW, next = block + stride;
-    slot = q8_slot(page, h, next, c);
+  while (block < end) {
+    const int t0 = real(block) * kW, next = block + stride;
+    slot = q8_slot(page, h, real(next), c);
     floatx4 s[2];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
@@ -137,18 +154,21 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
     // the keys' registers are free: the next block's keys are on their way during the softmax and the value product,
     // its values during the next scores. Four waves on a SIMD do the rest; a second set of registers instead left
     // room for two
-    if (next < nblk) load_keys(slot);
+    if (next < end) load_keys(slot);
     float mx = -__builtin_inff();
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[tb][e] *= sc;
-    if (t0 + kW > vis_first) {  // a token that some row of the tile does not see
+    // a token that some row of the tile does not see
+    if (t0 + kW > vis_first || (kSpan != kQ8Full && t0 < from_most && t0 + kW > p.sinks)) {
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (t0 + 16 * tb + 4 * g + e >= vis) s[tb][e] = -__builtin_inff();
+        for (int e = 0; e < 4; ++e) {
+          const int t = t0 + 16 * tb + 4 * g + e;
+          if (t >= vis || (kSpan != kQ8Full && t < from && t >= p.sinks)) s[tb][e] = -__builtin_inff();
+        }
     }
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
@@ -185,8 +205,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
       acc[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(v[j].x, v[j].y), wop, acc[2 * j], 0, 0, 0);
       acc[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<kFmt>(v[j].z, v[j].w), wop, acc[2 * j + 1], 0, 0, 0);
     }
-    if (next < nblk) load_values(slot);
-    page = q8_page(row, next + stride, c);
+    if (next < end) load_values(slot);
+    page = q8_page(row, real(next + stride), c);
     block = next;
   }
 
@@ -217,26 +237,19 @@ __global__ __launch_bounds__(kThreads, 4) void k_q8_split(Q8AttendArgs p) {
     lt += wl[w][cc] * __builtin_amdgcn_exp2f(wm[w][cc] - mt);
     o += *reinterpret_cast<const floatx4*>(&cmb[w][cc * kCombineRow + ch]) * __builtin_amdgcn_exp2f(wM[w][cc] - Mt);
   }
-  if (mine.records == 0) {
+  if (kSpan != kQ8Tree && mine.records == 0) {
     const RowFactor f(Mt, mt, lt);
     *reinterpret_cast<uint2*>(p.out + (((int64_t)b * c.Hq + chq) * p.n_max + ci) * kD + ch) =
         make_uint2(row_pack<kBf16>(f(o[0]), f(o[1])), row_pack<kBf16>(f(o[2]), f(o[3])));
     return;
   }
-  float* rec = p.ws + (int64_t)(mine.first * c.H + h * mine.records + tile * nsplit + split) * kRecFloatsQ8;
+  int64_t at = mine.first * c.H + h * mine.records + tile * nsplit + split;
+  if (kSpan == kQ8Tree && mine.records == 0) at = p.single + ((int64_t)b * c.H + h) * ntile + tile;
+  float* rec = p.ws + at * kRecFloatsQ8;
   *reinterpret_cast<floatx4*>(rec + cc * kD + ch) = o;
   if ((tid & 31) == 0) *reinterpret_cast<floatx4*>(rec + kQ8Cols * kD + 4 * cc) = floatx4{Mt, mt, lt, 0.0f};
 }
 
-// op over the 32 lanes of a half wave, in every lane of it
-template <typename Op>
-__device__ __forceinline__ float half_reduce(float v, Op&& op) {
-  v = op(v, fdpp<0xB1>(v));
-  v = op(v, fdpp<0x4E>(v));
-  v = op(v, fswap4(v));
-  v = op(v, fswap8(v));
-  return op(v, fswap16(v));
-}
 // Join the splits: kGroups groups of 32 lanes share a column's (a group takes every kGroups-th split, then the
 // groups are added), kCols columns a work-group
 template <bool kBf16, int kGroups, int kCols>
@@ -318,25 +331,34 @@ static void merge(const Q8AttendArgs& a, const Q8Plan& p, bool bf16, hipStream_t
   else hipLaunchKernelGGL((k_q8_merge<false, kGroups, kCols>), grid, block, 0, s, a, p.cols);
 }
 
-hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s) {
+template <int kSpan>
+static void split(const Q8AttendArgs& a, const Q8Plan& p, int format, bool bf16, hipStream_t s) {
+  const dim3 grid(p.splits.order.most, a.c.H * p.ntile, q8_layers(p)), block(kThreads);
+  if (format == OKVQ_Q8_INT8) {
+    if (bf16) hipLaunchKernelGGL((k_q8_split<kSpan, OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_q8_split<kSpan, OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
+  } else {
+    if (bf16) hipLaunchKernelGGL((k_q8_split<kSpan, OKVQ_Q8_E4M3, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_q8_split<kSpan, OKVQ_Q8_E4M3, false>), grid, block, 0, s, a);
+  }
+}
+
+hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s) {
   a.ntile = p.ntile;
   a.splits = p.splits;
   const bool bf16 = dtype == OKVQ_BF16;
   hipError_t e;
   if (p.cols != kQ8Cols) {
-    e = launch_q8_prompt(a, p, format, dtype, s);
+    e = launch_q8_prompt(a, p, span, format, dtype, s);
   } else {
-    const dim3 grid(p.splits.order.most, a.c.H * p.ntile, q8_layers(p)), block(kThreads);
-    if (format == OKVQ_Q8_INT8) {
-      if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_INT8, false>), grid, block, 0, s, a);
-    } else {
-      if (bf16) hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((k_q8_split<OKVQ_Q8_E4M3, false>), grid, block, 0, s, a);
-    }
+    if (span == kQ8Full) split<kQ8Full>(a, p, format, bf16, s);
+    else if (span == kQ8Window) split<kQ8Window>(a, p, format, bf16, s);
+    else split<kQ8Tree>(a, p, format, bf16, s);
     e = hipGetLastError();
   }
-  if (e != hipSuccess || p.splits.order.most == 1) return e;
+  if (e != hipSuccess) return e;
+  if (span == kQ8Tree) return launch_q8_tree_merge(a, p, dtype, s);
+  if (p.splits.order.most == 1) return e;
   // a column to 8 groups of lanes, 16 where there are many splits (128 splits: 7.9 -> 4.5 us); 8 columns to a work-group
   // where there are few (2 splits of 32768 rows: 33 -> 8 us)
   if (p.splits.order.most > 64) merge<16, 1>(a, p, bf16, s);

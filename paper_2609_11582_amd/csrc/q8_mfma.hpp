@@ -57,6 +57,51 @@ struct RowFactor {
   __device__ __forceinline__ float operator()(float v) const { return ldexpf(v * f, e); }
 };
 
+// op over the 32 lanes of a half wave, in every lane of it
+template <typename Op>
+__device__ __forceinline__ float half_reduce(float v, Op&& op) {
+  v = op(v, fdpp<0xB1>(v));
+  v = op(v, fdpp<0x4E>(v));
+  v = op(v, fswap4(v));
+  v = op(v, fswap8(v));
+  return op(v, fswap16(v));
+}
+
+// Tokens that a row i of n sees: those before `end`, and of them, with a window, those of the sinks and from `from` on
+struct Q8Sight {
+  int end, from;
+};
+// Bits of the drafts 32 word .. of n in a mask
+__device__ __forceinline__ uint32_t q8_named(uint32_t bits, int word, int n) {
+  const int left = n - 32 * word;
+  return left >= 32 ? bits : left > 0 ? bits & ((1u << left) - 1) : 0u;
+}
+template <int kSpan>
+__device__ __forceinline__ Q8Sight q8_sight(const Q8AttendArgs& p, int b, int len, int n, int i) {
+  Q8Sight s{len, 0};
+  if constexpr (kSpan == kQ8Window) {
+    s.end = max(len - n + i + 1, 0);
+    s.from = max(s.end - p.window, 0);
+  } else if constexpr (kSpan == kQ8Tree) {
+    // the row's place is behind the cache and the drafts of its line
+    if (p.window < len + n) {
+      const uint32_t* mask = p.visible + ((int64_t)b * p.n_max + i) * p.words;
+      int named = 0;
+      for (int w = 0; 32 * w < n; ++w) named += __builtin_popcount(q8_named(mask[w], w, n));
+      s.from = max(len + named - p.window, 0);
+    }
+  }
+  return s;
+}
+// The least and the largest `from` of rows first .. last
+template <int kSpan>
+__device__ __forceinline__ int q8_from_least(const Q8AttendArgs& p, int len, int n, int first) {
+  return kSpan == kQ8Window ? max(len - n + first + 1 - p.window, 0) : kSpan == kQ8Tree ? max(len - p.window, 0) : 0;
+}
+template <int kSpan>
+__device__ __forceinline__ int q8_from_most(const Q8AttendArgs& p, int len, int n, int last) {
+  return kSpan == kQ8Window ? max(len - n + last + 1 - p.window, 0) : kSpan == kQ8Tree ? max(len + n - p.window, 0) : 0;
+}
 // A lane's query channels as fp16 operands; returns the factor that belongs to the scores. fp16 rows enter as they
 // are. bfloat16 rows are scaled by a power of two that puts the row's largest magnitude into [2^14, 2^15): their
 // 8 bits fit fp16, and what lies 2^-29 or more below the largest is lost at most. row_max: the maximum over the lanes

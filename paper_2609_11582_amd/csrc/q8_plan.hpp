@@ -210,11 +210,41 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
   }
 }
 
+// The units (blocks or tiles of `size` tokens) that a tile of rows walks where they see the sinks, and the tokens from..end - 1:
+// those of the sinks, then those from the one that holds `from` on
+struct Q8Walk {
+  int sinks, skip, count;  // units of the sinks, units left out behind them, units in all
+  constexpr Q8Walk(int sink_tokens, int from, int end, int size) : sinks(0), skip(0), count((end + size - 1) / size) {
+    const int s = (sink_tokens + size - 1) / size, gap = from / size;
+    sinks = s < count ? s : count;
+    skip = gap > sinks ? (gap < count ? gap : count) - sinks : 0;
+    count -= skip;
+  }
+  constexpr int operator()(int i) const { return i < sinks ? i : i + skip; }
+};
+
+// Tokens that a tile of a slot's rows walks where they see the sinks and a window: what the plan counts in place of its length
+inline int q8_span(int len, int n_new, int G, int window, int sinks) {
+  const int64_t positions = std::min<int64_t>(n_new, kQ8PromptCols / G + 1);
+  return (int)std::min<int64_t>(len, (int64_t)sinks + window + positions + 2 * 32);  // window and sinks may begin and end inside blocks
+}
+
 // Split records of every call of up to n_max rows. A call's splits fit into its groups, but for units (tiles of a sequence
 // and head) that are more than the groups: those have one split and no record. Calls of few rows and of many count by themselves
 inline size_t q8_workspace_bound(int G, int n_max) {
   const size_t few = (size_t)kQ8Groups * kQ8Cols, many = (size_t)kQ8PromptGroups * kQ8PromptCols;
   return ((int64_t)n_max * G > kFewRows ? std::max(few, many) : few) * kQ8Record * sizeof(float);
+}
+
+// A tree's records: those of the splits, then one for each tile of each slot and head that has one split
+inline int64_t q8_split_records(const Q8Plan& p, int H) { return (int64_t)(p.splits.part[p.splits.order.split_slots] & 0xffffu) * H; }
+inline size_t q8_tree_workspace(const Q8Plan& p, int H) {
+  return (q8_split_records(p, H) + (int64_t)p.splits.order.slots * H * p.ntile) * p.cols * kQ8Record * sizeof(float);
+}
+// and of every call of up to n_max rows: the tiles of 16 columns, or of up to 256 where there are more than kFewRows rows
+inline size_t q8_tree_workspace_bound(int B, int H, int G, int n_max) {
+  const int64_t rows = (int64_t)n_max * G, cols = rows > kFewRows ? kQ8PromptCols : kQ8Cols;
+  return q8_workspace_bound(G, n_max) + (size_t)B * H * ((rows + cols - 1) / cols * cols) * kQ8Record * sizeof(float);
 }
 
 }  // namespace okvq

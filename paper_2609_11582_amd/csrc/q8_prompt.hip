@@ -33,7 +33,7 @@ struct Raw {                              // a thread's 16 bytes of keys or of v
   int block[kPieces], page[kPieces];
 };
 
-template <int kFmt, bool kBf16, int kWaves>
+template <int kSpan, int kFmt, bool kBf16, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, int width) {
   constexpr int kCols = 32 * kWaves, kPieces = 8 / kWaves;
   // two buffers of keys [block][16 channels][half h, token: at token ^ (channels & 7)] and of values
@@ -61,15 +61,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   const int r0 = tile * kCols, i_first = r0 / p.G;
   if (i_first >= n) return;
   const int i_last = min((r0 + kCols - 1) / p.G, n - 1);
-  const int vis_last = p.cross ? len : max(len - n + i_last + 1, 0);
+  auto cross = [&] { return kSpan == kQ8Tree || (kSpan == kQ8Full && p.cross); };
+  const int vis_last = cross() ? len : max(len - n + i_last + 1, 0);
   // the wave's columns, and the tokens that they see
   const int r = r0 + 32 * wave + col, i = r / p.G, hq = h * p.G + (r - i * p.G);
   const bool live = i < n;
-  const int vis = live ? (p.cross ? len : max(len - n + i + 1, 0)) : 0;
+  const int vis = live ? (cross() ? len : max(len - n + i + 1, 0)) : 0;
   const int wave_first = (r0 + 32 * wave) / p.G;
-  const int vis_first = wave_first >= n ? 0 : p.cross ? len : max(len - n + wave_first + 1, 0);
+  const int vis_first = wave_first >= n ? 0 : cross() ? len : max(len - n + wave_first + 1, 0);
   const bool busy = wave_first < n;  // a wave without a live column has only its part of the tiles to bring
-  const int steps = (vis_last + kTile - 1) / kTile;
+  // with a window the tiles are numbered over those that some row of the work-group sees
+  const Q8Walk walk(kSpan == kQ8Full ? 0 : p.sinks, q8_from_least<kSpan>(p, len, n, i_first), vis_last, kTile);
+  auto real = [&](int t) { return kSpan == kQ8Full ? t : walk(t); };
+  const int from_most = q8_from_most<kSpan>(p, len, n, min((r0 + 32 * wave + 31) / p.G, n - 1));
+  const int from = kSpan != kQ8Full && live ? q8_sight<kSpan>(p, b, len, n, i).from : 0;
+  const int steps = kSpan == kQ8Full ? (vis_last + kTile - 1) / kTile : walk.count;
   const int per = (steps + nsplit - 1) / nsplit, t_begin = min(split * per, steps), t_end = min(t_begin + per, steps);
 
   // Staging: a thread has 16 bytes of key row tid / 8 % 32 and of value slot tid % 256 of kPieces of the tile's two blocks.
@@ -82,7 +88,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   auto fetch_page = [&](int t, Raw<kPieces>& r) {
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
-      r.block[e] = min(2 * t + sb + e, last);
+      r.block[e] = min(2 * real(t) + sb + e, last);
       r.page[e] = uniform_load(table + min(r.block[e] >> c.bshift, c.max_pages - 1));
     }
   };
@@ -212,13 +218,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
       __syncthreads();
       continue;
     }
-    const int cur = u & 1, t0 = (t_begin + u) * kTile;
-    if (t0 + kTile > vis_first) {  // a token that some column of the wave does not see
+    const int cur = u & 1, t0 = real(t_begin + u) * kTile;
+    // a token that some column of the wave does not see
+    if (t0 + kTile > vis_first || (kSpan != kQ8Full && t0 < from_most && t0 + kTile > p.sinks)) {
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (t0 + tb * kW + 8 * (e >> 2) + 4 * half + (e & 3) >= vis) s[tb][e] = -__builtin_inff();
+        for (int e = 0; e < 16; ++e) {
+          const int t = t0 + tb * kW + 8 * (e >> 2) + 4 * half + (e & 3);
+          if (t >= vis || (kSpan != kQ8Full && t < from && t >= p.sinks)) s[tb][e] = -__builtin_inff();
+        }
       tops(s);
     }
     float sc[2], lv[2], high[2], reach[2], off[2], gain[2];
@@ -297,7 +306,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
 
   l = sum32(l);
   if (!live) return;
-  if (mine.records == 0) {
+  if (kSpan != kQ8Tree && mine.records == 0) {
     const RowFactor f(M, m, l);
     uint16_t* out = p.out + (((int64_t)b * c.Hq + hq) * p.n_max + i) * kD + 4 * half;
 #pragma unroll
@@ -308,7 +317,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
                                                                      row_pack<kBf16>(f(acc[j][e + 2]), f(acc[j][e + 3])));
     return;
   }
-  float* rec = p.ws + (int64_t)(mine.first * c.H + h * mine.records + tile * nsplit + split) * (kCols * kQ8Record);
+  int64_t place = mine.first * c.H + h * mine.records + tile * nsplit + split;
+  if (kSpan == kQ8Tree && mine.records == 0) place = p.single + ((int64_t)b * c.H + h) * ntile + tile;
+  float* rec = p.ws + place * (kCols * kQ8Record);
   const int cc = 32 * wave + col;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -321,17 +332,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
 
 }  // namespace
 
-template <int kFmt, bool kBf16>
+template <int kSpan, int kFmt, bool kBf16>
 static void launch(const Q8AttendArgs& a, const Q8Plan& p, hipStream_t s) {
   const int width = q8_layers(p) * a.c.H * p.ntile;
   const dim3 grid((unsigned)width, p.splits.order.most);
-  if (p.cols == 256) hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 8>), grid, dim3(512), 0, s, a, width);
-  else hipLaunchKernelGGL((k_q8_prompt<kFmt, kBf16, 4>), grid, dim3(256), 0, s, a, width);
+  if (p.cols == 256) hipLaunchKernelGGL((k_q8_prompt<kSpan, kFmt, kBf16, 8>), grid, dim3(512), 0, s, a, width);
+  else hipLaunchKernelGGL((k_q8_prompt<kSpan, kFmt, kBf16, 4>), grid, dim3(256), 0, s, a, width);
 }
 
-hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int format, int dtype, hipStream_t s) {
-  if (format == OKVQ_Q8_INT8) dtype == OKVQ_BF16 ? launch<OKVQ_Q8_INT8, true>(a, p, s) : launch<OKVQ_Q8_INT8, false>(a, p, s);
-  else dtype == OKVQ_BF16 ? launch<OKVQ_Q8_E4M3, true>(a, p, s) : launch<OKVQ_Q8_E4M3, false>(a, p, s);
+template <int kSpan>
+static void launch(const Q8AttendArgs& a, const Q8Plan& p, int format, bool bf16, hipStream_t s) {
+  if (format == OKVQ_Q8_INT8) bf16 ? launch<kSpan, OKVQ_Q8_INT8, true>(a, p, s) : launch<kSpan, OKVQ_Q8_INT8, false>(a, p, s);
+  else bf16 ? launch<kSpan, OKVQ_Q8_E4M3, true>(a, p, s) : launch<kSpan, OKVQ_Q8_E4M3, false>(a, p, s);
+}
+
+hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s) {
+  if (span == kQ8Full) launch<kQ8Full>(a, p, format, dtype == OKVQ_BF16, s);
+  else if (span == kQ8Window) launch<kQ8Window>(a, p, format, dtype == OKVQ_BF16, s);
+  else launch<kQ8Tree>(a, p, format, dtype == OKVQ_BF16, s);
   return hipGetLastError();
 }
 

@@ -67,6 +67,9 @@ def lib() -> ctypes.CDLL:
                 ("okvq_q8_append", i32, [P(Q8Struct), i32, vp, vp, vp, vp, vp, i32, vp]),
                 ("okvq_q8_workspace_bytes", sz, [P(Q8Dims), i32, i32]),
                 ("okvq_q8_attention", i32, [P(Q8Struct), i32, vp, vp, vp, vp, i32, ctypes.c_float, vp, vp, sz, u32, vp]),
+                ("okvq_q8_window_attention", i32, [P(Q8Struct), i32, vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, sz, vp]),
+                ("okvq_q8_tree_workspace_bytes", sz, [P(Q8Dims), i32]),
+                ("okvq_q8_tree_attention", i32, [P(Q8Struct), i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, vp, vp, sz, vp]),
                 ("okvq_q8_page_workspace_bytes", sz, [P(Q8Dims)]),
                 ("okvq_q8_extend", i32, [P(Q8Struct), vp, vp, vp, sz, vp]),
                 ("okvq_q8_fork", i32, [P(Q8Struct), vp, vp, i32, vp]),
@@ -368,6 +371,69 @@ def okvq_q8_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, s
                                  _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_q8_attention")
+    return st
+
+
+def okvq_q8_window_attention(cache: Q8Cache, layer, lens, q, n_new, n_new_dev, n_max, window, sinks, sm_scale, out, workspace,
+                             stream=None, check=True) -> int:
+    """okvq_q8_attention of rows that see the newest `window` tokens up to their own and the first `sinks`; its workspace."""
+    B, _, Hq = cache._sizes
+    dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
+    shape = (B, Hq, n_max, 128)
+    st = lib().okvq_q8_window_attention(
+        _cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need_rows(q, shape, dt, "q", dev), _ints(n_new, B, "n_new"),
+        _need(n_new_dev, B * 4, torch.int32, "n_new_dev", dev), n_max, _int(window, "window"), _int(sinks, "sinks"), float(sm_scale),
+        _need_rows(out, shape, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes, _stream(stream))
+    if check and st:
+        _check(st, "okvq_q8_window_attention")
+    return st
+
+
+def okvq_q8_tree_workspace_bytes(dims: Q8Dims, n_max: int) -> int:
+    return lib().okvq_q8_tree_workspace_bytes(ctypes.byref(dims), _int(n_max, "n_max"))
+
+
+def q8_tree_workspace(dims: Q8Dims, n_max: int, device="cuda") -> torch.Tensor:
+    """A workspace of okvq_q8_tree_workspace_bytes bytes for okvq_q8_tree_attention (no contents needed)."""
+    return torch.empty(max(okvq_q8_tree_workspace_bytes(dims, n_max) + 15, 16) // 16 * 4, dtype=torch.float32, device=device)
+
+
+def q8_tree_visible(parents: Sequence[Sequence[int]], n_max: int, device="cuda") -> torch.Tensor:
+    """Masks int32 [batch][n_max][ceil(n_max / 32)] for okvq_q8_tree_attention: of each slot, the parent of every draft, an
+    earlier draft or -1 for one that follows the cache."""
+    words = -(-n_max // 32)
+    flat = []
+    for b, slot in enumerate(parents):
+        if len(slot) > n_max:
+            raise ValueError(f"parents[{b}]: {len(slot)} drafts, at most {n_max}")
+        masks = []
+        for i, parent in enumerate(slot):
+            if not -1 <= parent < i:
+                raise ValueError(f"parents[{b}][{i}]: {parent}, expected -1 or an earlier draft")
+            masks.append((masks[parent] if parent >= 0 else 0) | 1 << i)
+        for mask in masks + [0] * (n_max - len(slot)):
+            for w in range(words):
+                bits = mask >> 32 * w & 0xffffffff
+                flat.append(bits - (1 << 32) if bits >> 31 else bits)
+    return torch.tensor(flat, dtype=torch.int32).view(len(parents), n_max, words).to(device)
+
+
+def okvq_q8_tree_attention(cache: Q8Cache, layer, lens, q, k_draft, v_draft, visible, n_draft, n_draft_dev, n_max, sm_scale, out,
+                           workspace, window=0, sinks=0, stream=None, check=True) -> int:
+    """Attention of drafts that are not in the cache: rows q, out [B][Hq][n_max][128] and k_draft, v_draft [B][H][n_max][128]
+    (contiguous); visible int32 [B][n_max][ceil(n_max / 32)], the drafts that each one sees (q8_tree_visible); lens: tokens
+    in the cache. window 0: all of them."""
+    B, H, Hq = cache._sizes
+    dev, dt, n_max = _device(), cache.row_dtype, _int(n_max, "n_max")
+    shape, drafts = (B, Hq, n_max, 128), (B, H, n_max, 128)
+    st = lib().okvq_q8_tree_attention(
+        _cache_ref(cache, dev), _int(layer, "layer"), _ints(lens, B, "lens"), _need_rows(q, shape, dt, "q", dev),
+        _need_rows(k_draft, drafts, dt, "k_draft", dev), _need_rows(v_draft, drafts, dt, "v_draft", dev),
+        _need_rows(visible, (B, n_max, -(-n_max // 32)), torch.int32, "visible", dev), _ints(n_draft, B, "n_draft"),
+        _need(n_draft_dev, B * 4, torch.int32, "n_draft_dev", dev), n_max, _int(window, "window"), _int(sinks, "sinks"), float(sm_scale),
+        _need_rows(out, shape, dt, "out", dev), _need(workspace, 0, None, "workspace", dev), workspace.nbytes, _stream(stream))
+    if check and st:
+        _check(st, "okvq_q8_tree_attention")
     return st
 
 

@@ -1,0 +1,75 @@
+// Host check of what a window and a tree add to the 8-bit attention's launch plan, with the mappings that its kernels use: a
+// walk meets every unit that a row sees once and in order and no unit that none does; a tree's records lie apart and inside
+// its workspace, which the stated bound covers. Prints "ok" or the first call that breaks a rule.
+#include "q8_plan.hpp"
+
+#include <climits>
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <set>
+#include <vector>
+
+using namespace okvq;
+
+static std::mt19937 rng(11);
+static int below(int n) { return (int)(rng() % (unsigned)n); }
+static int spread(int most) { return (int)std::exp2(std::log2(most + 1.0) * (rng() / 4294967296.0)); }
+static void fail(const char* what, long a, long b, long c, long d) {
+  std::printf("%s: %ld %ld %ld %ld\n", what, a, b, c, d);
+  std::exit(1);
+}
+
+int main() {
+  for (int call = 0; call < 200000; ++call) {
+    const int end = below(6) ? spread(3000) : 0, size = below(2) ? 32 : 64;
+    const int sinks = below(3) ? below(200) : below(2) ? 0 : 1 << 27, from = below(5) ? below(end + 40) : 0;
+    const Q8Walk w(sinks, from, end, size);
+    if (w.count < 0 || w.sinks < 0 || w.skip < 0) fail("negative", sinks, from, end, size);
+    int at = 0;
+    for (int u = 0; u * size < end; ++u) {
+      const int a = u * size, b = std::min(a + size, end);
+      const bool seen = a < sinks || (from < b && from < end);
+      if (seen && (at >= w.count || w(at) != u)) fail("unit", sinks, from, end, size);
+      at += seen;
+    }
+    // from behind the end: the unit that holds it may be walked, and is masked
+    if (at != w.count && !(from >= end && w.count <= at + 1)) fail("count", sinks, from, end, size);
+    for (int i = 0; i < w.count; ++i)
+      if (w(i) < 0 || w(i) * size >= end) fail("outside", sinks, from, end, size);
+  }
+  for (int call = 0; call < 4000; ++call) {
+    const int B = call % 3 == 0 ? 1 : 1 + spread(call % 3 == 1 ? 40 : 1023), H = 1 + spread(15), G = 1 + below(16), n_max = 1 + spread(255);
+    const int window = below(2) ? INT_MAX : 1 + spread(5000), sinks = below(2) ? 0 : spread(1 << 27);
+    std::vector<int32_t> lens(B), n_new(B), spans(B);
+    int most = 0;
+    for (int b = 0; b < B; ++b) {
+      lens[b] = below(8) ? spread(call % 5 ? 70000 : 1500) : 0;
+      n_new[b] = below(4) ? 1 + below(n_max) : 0;
+      most = std::max(most, n_new[b]);
+      spans[b] = q8_span(lens[b], n_new[b], G, window, sinks);
+      if (spans[b] < 0 || spans[b] > lens[b]) fail("span", lens[b], spans[b], window, sinks);
+      if (window == INT_MAX && spans[b] != lens[b]) fail("whole span", lens[b], spans[b], window, sinks);
+    }
+    if (most == 0) continue;
+    Q8Plan p;
+    q8_plan(p, B, H, G, most, spans.data(), n_new.data());
+    const int64_t single = q8_split_records(p, H), all = (int64_t)q8_tree_workspace(p, H) / sizeof(float) / ((int64_t)p.cols * kQ8Record);
+    if (q8_tree_workspace(p, H) > q8_tree_workspace_bound(B, H, G, n_max)) fail("bound", B, H, G, most);
+    if (single * p.cols > (int64_t)q8_workspace_bound(G, most) / 4 / kQ8Record) fail("split records", B, H, G, most);
+    std::set<int64_t> met;
+    for (int place = 0; place < B; ++place)
+      for (int tile = 0; tile < p.ntile; ++tile) {
+        const Q8Part w = q8_part(p.splits.order, p.splits.part[q8_part_index(place)], p.splits.part[q8_part_index(place) + 1], place, 0, tile);
+        const int b = p.splits.order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
+        for (int h = 0; h < H; ++h)
+          for (int split = 0; split < w.nsplit; ++split) {
+            int64_t at = w.first * H + h * w.records + tile * w.nsplit + split;
+            if (w.records == 0) at = single + ((int64_t)b * H + h) * p.ntile + tile;
+            if (at < 0 || at >= all || (w.records && at >= single) || !met.insert(at).second) fail("record", B, H, G, most);
+          }
+      }
+  }
+  std::printf("ok\n");
+}
