@@ -221,6 +221,10 @@ struct Q8Walk {
     count -= skip;
   }
   constexpr int operator()(int i) const { return i < sinks ? i : i + skip; }
+  constexpr int before(int end, int size) const {  // units of the walk with tokens before `end`
+    const int n = (end + size - 1) / size;
+    return n <= sinks ? n : n - skip > sinks ? n - skip : sinks;
+  }
 };
 
 // Tokens that a tile of a slot's rows walks where they see the sinks and a window: what the plan counts in place of its length

@@ -70,12 +70,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   const int wave_first = (r0 + 32 * wave) / p.G;
   const int vis_first = wave_first >= n ? 0 : cross() ? len : max(len - n + wave_first + 1, 0);
   const bool busy = wave_first < n;  // a wave without a live column has only its part of the tiles to bring
-  // with a window the tiles are numbered over those that some row of the work-group sees
-  const Q8Walk walk(kSpan == kQ8Full ? 0 : p.sinks, q8_from_least<kSpan>(p, len, n, i_first), vis_last, kTile);
-  auto real = [&](int t) { return kSpan == kQ8Full ? t : walk(t); };
-  const int from_most = q8_from_most<kSpan>(p, len, n, min((r0 + 32 * wave + 31) / p.G, n - 1));
+  // with a window the blocks are numbered over those that some row of the work-group sees, and a tile is two in a row of these
+  const Q8Walk walk(kSpan == kQ8Full ? 0 : p.sinks, q8_from_least<kSpan>(p, len, n, i_first), vis_last, kW);
+  const int steps = kSpan == kQ8Full ? (vis_last + kTile - 1) / kTile : (walk.count + 1) / 2;
+  // what the wave's rows see at most, and where the last of them begins
+  const int wave_last = min((r0 + 32 * wave + 31) / p.G, n - 1);
+  const int vis_most = cross() ? len : max(len - n + wave_last + 1, 0);
+  const int from_most = q8_from_most<kSpan>(p, len, n, wave_last);
   const int from = kSpan != kQ8Full && live ? q8_sight<kSpan>(p, b, len, n, i).from : 0;
-  const int steps = kSpan == kQ8Full ? (vis_last + kTile - 1) / kTile : walk.count;
   const int per = (steps + nsplit - 1) / nsplit, t_begin = min(split * per, steps), t_end = min(t_begin + per, steps);
 
   // Staging: a thread has 16 bytes of key row tid / 8 % 32 and of value slot tid % 256 of kPieces of the tile's two blocks.
@@ -88,7 +90,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
   auto fetch_page = [&](int t, Raw<kPieces>& r) {
 #pragma unroll
     for (int e = 0; e < kPieces; ++e) {
-      r.block[e] = min(2 * real(t) + sb + e, last);
+      r.block[e] = min(kSpan == kQ8Full ? 2 * t + sb + e : walk(2 * t + sb + e), last);
       r.page[e] = uniform_load(table + min(r.block[e] >> c.bshift, c.max_pages - 1));
     }
   };
@@ -210,25 +212,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
     load_values(t_begin + u + 2, vr);
     load_keys(t_begin + u + 3, kr);
   };
-  for (int u = 0; u < nt; ++u) {
+  // with a window a wave stops at the last tile that its rows see, and only stages those for other waves' rows
+  int u = 0, own = nt;
+  if constexpr (kSpan != kQ8Full) own = busy ? min(max((walk.before(vis_most, kW) + 1) / 2 - t_begin, 0), nt) : 0;
+  for (; u < own; ++u) {
     fetched(kr);
     fetched(vr);
-    if (!busy) {
+    if (kSpan == kQ8Full && !busy) {
       stage(u);
       __syncthreads();
       continue;
     }
-    const int cur = u & 1, t0 = real(t_begin + u) * kTile;
-    // a token that some column of the wave does not see
-    if (t0 + kTile > vis_first || (kSpan != kQ8Full && t0 < from_most && t0 + kTile > p.sinks)) {
+    const int cur = u & 1;
+    if constexpr (kSpan == kQ8Full) {
+      const int t0 = (t_begin + u) * kTile;
+      if (t0 + kTile > vis_first) {  // a token that some column of the wave does not see
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
+        for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int t = t0 + tb * kW + 8 * (e >> 2) + 4 * half + (e & 3);
-          if (t >= vis || (kSpan != kQ8Full && t < from && t >= p.sinks)) s[tb][e] = -__builtin_inff();
+          for (int e = 0; e < 16; ++e)
+            if (t0 + tb * kW + 8 * (e >> 2) + 4 * half + (e & 3) >= vis) s[tb][e] = -__builtin_inff();
+        tops(s);
+      }
+    } else {
+      const int base[2] = {walk(2 * (t_begin + u)) * kW, walk(2 * (t_begin + u) + 1) * kW};
+      bool edge = false;
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb) {
+        const int t0 = base[tb], vis_at = vis - t0 - 4 * half, from_at = from - t0 - 4 * half;
+        if (t0 + kW > vis_first) {
+          edge = true;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (8 * (e >> 2) + (e & 3) >= vis_at) s[tb][e] = -__builtin_inff();
         }
-      tops(s);
+        if (t0 < from_most && t0 + kW > p.sinks) {
+          edge = true;
+          const int sinks_at = p.sinks - t0 - 4 * half;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (8 * (e >> 2) + (e & 3) < from_at && 8 * (e >> 2) + (e & 3) >= sinks_at) s[tb][e] = -__builtin_inff();
+        }
+      }
+      if (edge) tops(s);
     }
     float sc[2], lv[2], high[2], reach[2], off[2], gain[2];
     bool dead[2] = {false, false};
@@ -303,6 +329,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_q8_prompt(Q8AttendArgs p, in
     tops(s);
     __syncthreads();
   }
+  if constexpr (kSpan != kQ8Full)
+    for (; u < nt; ++u) {
+      fetched(kr);
+      fetched(vr);
+      stage(u);
+      __syncthreads();
+    }
 
   l = sum32(l);
   if (!live) return;

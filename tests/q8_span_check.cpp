@@ -36,6 +36,10 @@ int main() {
     }
     // from behind the end: the unit that holds it may be walked, and is masked
     if (at != w.count && !(from >= end && w.count <= at + 1)) fail("count", sinks, from, end, size);
+    const int part = below(end + 1);
+    int n = 0;
+    while (n < w.count && w(n) * size < part) ++n;
+    if (w.before(part, size) != n) fail("before", sinks, from, part, size);
     for (int i = 0; i < w.count; ++i)
       if (w(i) < 0 || w(i) * size >= end) fail("outside", sinks, from, end, size);
   }
