@@ -15,7 +15,7 @@ LIB = os.path.join(PKG, "libokvq.so")
 SOURCES = ["api.hip", "codec_kernels.hip", "codec_fused.hip", "decode_kernels.hip", "calib_kernels.hip",
            "dense_decode.hip", "ladder_codec.hip", "ladder_decode.hip", "append_window.hip", "codec_block.hip",
            "rotary.hip", "norm_rotary.hip", "q8_api.hip", "q8_append.hip", "q8_attention.hip", "q8_prompt.hip",
-           "q8_tree.hip", "q8_pages.hip"]
+           "q8_wide.hip", "q8_tree.hip", "q8_pages.hip"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
@@ -40,7 +40,8 @@ def hipcc() -> str:
 # value they use), so min / max need no NaN quieting
 EXTRA = {"decode_kernels.hip": ["-fno-honor-nans"], "dense_decode.hip": ["-fno-honor-nans"],
          "ladder_decode.hip": ["-fno-honor-nans"], "q8_attention.hip": ["-fno-honor-nans"],
-         "q8_prompt.hip": ["-fno-honor-nans"], "q8_tree.hip": ["-fno-honor-nans"], "q8_append.hip": ["-fno-honor-nans"],
+         "q8_prompt.hip": ["-fno-honor-nans"], "q8_wide.hip": ["-fno-honor-nans"],
+         "q8_tree.hip": ["-fno-honor-nans"], "q8_append.hip": ["-fno-honor-nans"],
          # the codecs take window minima and maxima of finite directions (finite inputs are part of the device data
          # contract): no NaN quieting around them
          "append_window.hip": ["-fno-honor-nans"], "codec_fused.hip": ["-fno-honor-nans"],

@@ -83,6 +83,7 @@ struct Q8AttendArgs {
 // of these the sinks and a window; or what precedes a tree of drafts (all, or sinks and window), whose part a merge adds
 constexpr int kQ8Full = 0, kQ8Window = 1, kQ8Tree = 2;
 hipError_t launch_q8_prompt(const Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s);
+hipError_t launch_q8_wide(const Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s);
 hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int span, int format, int dtype, hipStream_t s);
 hipError_t launch_q8_tree_merge(const Q8AttendArgs& a, const Q8Plan& p, int dtype, hipStream_t s);
 

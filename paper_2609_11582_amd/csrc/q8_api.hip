@@ -229,12 +229,13 @@ okvq_status attend(Q8AttendArgs& a, int span, const okvq_q8_cache* cache, int32_
     for (int b = 0; b < d.batch; ++b) spans[b] = q8_span(lens_host[b], n_new_host[b], G, a.window, a.sinks);
   }
   Q8Plan plan;
-  q8_plan(plan, d.batch, d.num_kv_heads, G, most, span == kQ8Full ? lens_host : spans, n_new_host);
+  q8_plan(plan, d.batch, d.num_kv_heads, G, most, span == kQ8Full ? lens_host : spans, n_new_host, span);
   const size_t need = span == kQ8Tree ? q8_tree_workspace(plan, d.num_kv_heads) : q8_workspace_bound(G, most);
   if (!aligned16(workspace) || workspace_bytes < need) return OKVQ_ERR_WORKSPACE;
   const int64_t units = (int64_t)plan.ntile * d.num_kv_heads;
   if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
       (plan.splits.order.most > 1 && (!launchable(units * plan.splits.order.split_slots * 32, 256) || units > 65535)) ||
+      (plan.cols == kQ8WideCols && !launchable(q8_wide_groups(plan, d.num_kv_heads), 512)) ||
       (span == kQ8Tree && (!launchable(units * d.batch * plan.rows, 512) || units > 65535)))
     return OKVQ_ERR_UNSUPPORTED;
   a.c = view(cache, layer);

@@ -348,7 +348,9 @@ hipError_t launch_q8_attention(Q8AttendArgs& a, const Q8Plan& p, int span, int f
   a.splits = p.splits;
   const bool bf16 = dtype == OKVQ_BF16;
   hipError_t e;
-  if (p.cols != kQ8Cols) {
+  if (p.cols == kQ8WideCols) {
+    e = launch_q8_wide(a, p, span, format, dtype, s);
+  } else if (p.cols != kQ8Cols) {
     e = launch_q8_prompt(a, p, span, format, dtype, s);
   } else {
     if (span == kQ8Full) split<kQ8Full>(a, p, format, bf16, s);

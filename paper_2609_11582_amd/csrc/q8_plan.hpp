@@ -11,6 +11,7 @@ namespace okvq {
 
 constexpr int kQ8MaxBatch = 1024;    // slots: one thread each in the page kernels
 constexpr int kQ8Cols = 16;          // query columns of a tile of the split kernel
+constexpr int kQ8WideCols = 64;      // of the wide kernel (a window's or a tree's rows)
 constexpr int kQ8PromptCols = 256;   // and of the prompt kernel at most
 constexpr int kQ8MaxSplits = 128;
 constexpr int kQ8Groups = 512;       // work-groups that a call of few rows is split into
@@ -96,7 +97,66 @@ inline int q8_layers(const Q8Plan& p) {
   return o.split_slots + (o.slots - o.split_slots + o.most - 1) / o.most;
 }
 
+// Wide kernel, launched as one row of work-groups: the splits of the plan, dealt to the 8 XCDs (which take work-groups in turn) in
+// even shares whose neighbours are tiles of one split, then the tiles that have one split: of all slots, or, where every split
+// slot has all tiles split, of the others
+struct Q8Units {
+  int split, per;      // work-groups that are splits, and of an XCD
+  int64_t singles;     // work-groups behind them
+  int first_single;    // place of the first slot that may have such tiles
+};
+struct Q8Unit {
+  int place = -1, h = 0, tile = 0;  // place < 0: nothing
+  int split = 0, nsplit = 1, records = 0, first = 0;  // as in Q8Part
+};
+inline Q8Units q8_units(const Q8Plan& p, int H) {
+  const Q8Order& o = p.splits.order;
+  Q8Units u;
+  u.split = (int)(p.splits.part[o.split_slots] & 0xffffu) * H;
+  u.per = (u.split + 7) / 8;
+  u.first_single = o.split_slots;
+  for (int i = 0; i < o.split_slots; ++i)
+    if ((int)((p.splits.part[i + 1] & 0xffffu) - (p.splits.part[i] & 0xffffu)) < (int)(p.splits.part[i] >> 16) * p.ntile) u.first_single = 0;
+  u.singles = (int64_t)(o.slots - u.first_single) * H * p.ntile;
+  return u;
+}
+inline int64_t q8_wide_groups(const Q8Plan& p, int H) {
+  const Q8Units u = q8_units(p, H);
+  return 8 * (int64_t)u.per + u.singles;
+}
+constexpr Q8Unit q8_unit(const Q8Splits& s, const Q8Units& units, int H, int ntile, int64_t id) {
+  Q8Unit u;
+  if (id < 8 * (int64_t)units.per) {
+    const int at = (int)(id & 7) * units.per + (int)(id >> 3);
+    if (at >= units.split) return u;
+    int lo = 0, hi = s.order.split_slots;  // the last slot whose splits begin at or before it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if ((int)(s.part[mid] & 0xffffu) * H <= at) lo = mid;
+      else hi = mid;
+    }
+    u.place = lo;
+    u.first = (int)(s.part[lo] & 0xffffu);
+    u.nsplit = (int)(s.part[lo] >> 16);
+    u.records = (int)(s.part[lo + 1] & 0xffffu) - u.first;
+    const int tiles = u.records / u.nsplit, local = at - u.first * H, rest = local / tiles;
+    u.tile = local - rest * tiles;
+    u.h = rest / u.nsplit;
+    u.split = rest - u.h * u.nsplit;
+    return u;
+  }
+  const int64_t at = id - 8 * (int64_t)units.per, unit = at / ntile;
+  const int tile = (int)(at - unit * ntile), place = units.first_single + (int)(unit / H);
+  if (place < s.order.split_slots && tile * (int)(s.part[place] >> 16) < (int)((s.part[place + 1] & 0xffffu) - (s.part[place] & 0xffffu)))
+    return u;  // split
+  u.place = place;
+  u.h = (int)(unit % H);
+  u.tile = tile;
+  return u;
+}
+
 constexpr int kFewRows = 32;  // rows of a head that always take the split kernel
+constexpr int kWideRows = 256; // and that take the wide kernel at most, where they see a window or precede a tree
 
 // Every split takes the same number of tokens at most, the least that needs no more work-groups than fit the GPU at
 // once: a ragged batch is shared evenly (16 sequences of 8704 to 16384 tokens: 46 -> 41 us against as many splits for each).
@@ -129,11 +189,11 @@ constexpr int kFewRows = 32;  // rows of a head that always take the split kerne
 //   81.7 -> 85.7, 200 even up to 16000 354 -> 348.
 // most_new: the most new rows of a slot, 1 at least.
 // Tiles of 256 columns x heads are below 2^23 a slot (checked before), so that no product here passes 64 bits.
-inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new) {
+inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new, int span = 0) {
   const int64_t rows = (int64_t)most_new * G;
   const auto tiles = [&](int b, int cols) { return ((int64_t)n_new[b] * G + cols - 1) / cols; };
   int longest = 0, active = 0, fewest = most_new;
-  int64_t units16 = 0, units256 = 0, work16 = 0;  // tiles of all heads, and tiles x tokens
+  int64_t units16 = 0, units64 = 0, units256 = 0, work16 = 0;  // tiles of all heads, and tiles x tokens
   for (int b = 0; b < B; ++b) {
     if (n_new[b] == 0) continue;
     ++active;
@@ -142,18 +202,22 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     units16 += n;
     if (units16 <= kQ8Groups) work16 += n * lens[b];
     fewest = std::min(fewest, n_new[b]);
-    if (rows > kFewRows) units256 += tiles(b, kQ8PromptCols) * H;
+    if (rows > kFewRows) {
+      units64 += tiles(b, kQ8WideCols) * H;
+      units256 += tiles(b, kQ8PromptCols) * H;
+    }
   }
   const int64_t launched = (rows + kQ8Cols - 1) / kQ8Cols * H * B;
   const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18 && launched <= 16 * kQ8Groups);
+  const bool wide = span != 0 && !few && rows <= kWideRows;
   const bool half = rows > 128 && longest <= 2048 && units256 <= 256;
-  p.cols = few ? kQ8Cols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
+  p.cols = few ? kQ8Cols : wide ? kQ8WideCols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
   p.rows = (int)std::min<int64_t>(rows, p.cols);
   const int64_t groups = few ? kQ8Groups : kQ8PromptGroups;
-  const int64_t round = few ? 256 : longest < 1024 ? 512 : 256;  // tokens of a round
-  int64_t units = few ? units16 : units256;
-  if (half) {
+  const int64_t round = few || wide ? 256 : longest < 1024 ? 512 : 256;  // tokens of a round
+  int64_t units = few ? units16 : wide ? units64 : units256;
+  if (half && !wide) {
     units = 0;
     for (int b = 0; b < B; ++b) units += tiles(b, p.cols) * H;
   }

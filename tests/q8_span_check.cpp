@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
+#include <cstring>
 #include <random>
 #include <set>
 #include <vector>
@@ -57,23 +58,60 @@ int main() {
       if (window == INT_MAX && spans[b] != lens[b]) fail("whole span", lens[b], spans[b], window, sinks);
     }
     if (most == 0) continue;
+    const int span = 1 + below(2);
     Q8Plan p;
-    q8_plan(p, B, H, G, most, spans.data(), n_new.data());
+    std::memset(&p, 0xff, sizeof(p));  // nothing may be read that the plan does not set
+    q8_plan(p, B, H, G, most, spans.data(), n_new.data(), span);
+    if (p.splits.order.split_slots + 1 > (int)(sizeof(p.splits.part) / 4)) fail("too many split slots", B, H, G, most);
     const int64_t single = q8_split_records(p, H), all = (int64_t)q8_tree_workspace(p, H) / sizeof(float) / ((int64_t)p.cols * kQ8Record);
     if (q8_tree_workspace(p, H) > q8_tree_workspace_bound(B, H, G, n_max)) fail("bound", B, H, G, most);
     if (single * p.cols > (int64_t)q8_workspace_bound(G, most) / 4 / kQ8Record) fail("split records", B, H, G, most);
-    std::set<int64_t> met;
+    // every slot, head, tile and split is met by one work-group
+    std::set<int64_t> met, done;
+    const auto meet = [&](int place, int x, int h, int tile) {
+      const Q8Part w = q8_part(p.splits.order, p.splits.part[q8_part_index(place)], p.splits.part[q8_part_index(place) + 1], place, x, tile);
+      if (w.none) return;
+      const int b = p.splits.order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
+      if (b >= B || w.split >= w.nsplit || w.nsplit > p.splits.order.most || h >= H || tile >= p.ntile) fail("range", B, H, G, most);
+      if (!done.insert((((int64_t)b * H + h) * p.ntile + tile) * p.splits.order.most + w.split).second) fail("twice", B, H, G, most);
+      int64_t at = w.first * H + h * w.records + tile * w.nsplit + w.split;
+      if (w.records == 0) at = single + ((int64_t)b * H + h) * p.ntile + tile;
+      if (at < 0 || at >= all || (w.records && at >= single) || !met.insert(at).second) fail("record", B, H, G, most);
+    };
+    const int width = q8_layers(p) * H * p.ntile;
+    for (int x = 0; x < p.splits.order.most; ++x)
+      if (p.cols == kQ8WideCols) {
+        const Q8Units units = q8_units(p, H);
+        for (int64_t id = 0; x == 0 && id < 8 * (int64_t)units.per + units.singles; ++id) {
+          const Q8Unit u = q8_unit(p.splits, units, H, p.ntile, id);
+          if (u.place < 0) continue;
+          const Q8Part w = q8_part(p.splits.order, p.splits.part[q8_part_index(u.place)], p.splits.part[q8_part_index(u.place) + 1], u.place, u.split, u.tile);
+          if (w.none || w.nsplit != u.nsplit || w.split != u.split || w.records != u.records || w.first != u.first) fail("unit", B, H, G, most);
+          meet(u.place, u.split, u.h, u.tile);
+        }
+      } else if (p.cols == kQ8Cols) {
+        for (int layer = 0; layer < q8_layers(p); ++layer)
+          for (int y = 0; y < H * p.ntile; ++y) meet(q8_place(p.splits.order, layer, x), x, y / p.ntile, y % p.ntile);
+      } else {
+        for (int w = 0; w < width; ++w) {
+          const Q8Tile t = q8_tile(p.splits.order, H, p.ntile, width, w, x);
+          if (t.place >= 0) meet(t.place, x, t.h, t.tile);
+        }
+      }
+    // and what the merge reads is what they wrote
     for (int place = 0; place < B; ++place)
       for (int tile = 0; tile < p.ntile; ++tile) {
         const Q8Part w = q8_part(p.splits.order, p.splits.part[q8_part_index(place)], p.splits.part[q8_part_index(place) + 1], place, 0, tile);
         const int b = p.splits.order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
+        if (w.nsplit > kQ8MaxSplits) fail("splits", B, H, G, most);
         for (int h = 0; h < H; ++h)
           for (int split = 0; split < w.nsplit; ++split) {
             int64_t at = w.first * H + h * w.records + tile * w.nsplit + split;
             if (w.records == 0) at = single + ((int64_t)b * H + h) * p.ntile + tile;
-            if (at < 0 || at >= all || (w.records && at >= single) || !met.insert(at).second) fail("record", B, H, G, most);
+            if (!met.erase(at)) fail("merge", B, H, G, most);
           }
       }
+    if (!met.empty()) fail("left over", B, H, G, most);
   }
   std::printf("ok\n");
 }
