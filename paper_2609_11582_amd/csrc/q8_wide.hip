@@ -54,7 +54,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
   __shared__ __attribute__((aligned(16))) char shared[sizeof(WideShared)];
   WideShared& sh = *reinterpret_cast<WideShared*>(shared);
   const Q8View& c = p.c;
-  const int ntile = p.ntile;
+  int ntile = p.ntile;
+  __asm__ volatile(""  // one wait for the arguments
+                   : "+s"(ntile)
+                   : "s"(c.k_codes), "s"(c.v_codes), "s"(c.k_scale), "s"(c.v_scale), "s"(c.table), "s"(c.lens), "s"(c.H), "s"(c.Hq), "s"(c.P),
+                     "s"(c.max_pages), "s"(c.bshift), "s"(p.q), "s"(p.n_new), "s"(p.n_max), "s"(p.G), "s"(p.window), "s"(p.sinks),
+                     "s"(p.splits.order.split_slots), "s"(p.splits.order.flags), "s"(p.splits.part[0]), "s"(units.split), "s"(units.per));
   const Q8Unit mine = q8_unit(p.splits, units, c.H, ntile, blockIdx.x);
   if (mine.place < 0) return;
   const int h = mine.h, tile = mine.tile, nsplit = mine.nsplit;
