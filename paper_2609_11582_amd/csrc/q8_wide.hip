@@ -174,7 +174,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
       for (int e = 0; e < 16; ++e) acc[ct][j][e] = 0.0f;
   }
 
+  // The two waves of a SIMD lead in turn: left alone the older one ends a third of its blocks earlier, and the younger one's last
+  // blocks run without a partner (8 slots of up to 25 drafts 34.4 -> 33.8 us)
+  int turn = wave >> 2;
   while (block < end) {
+    if ((turn ^= 1) == 0) __builtin_amdgcn_s_setprio(1);
+    else __builtin_amdgcn_s_setprio(0);
     __asm__ volatile("" ::: "memory");  // the query operands stay in LDS
     const int t0 = walk(block) * kW, next = block + stride;
     slot = q8_slot(page, h, walk(next), c);
@@ -283,6 +288,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
     page = q8_page(row, walk(next + stride), c);
     block = next;
   }
+
+  __builtin_amdgcn_s_setprio(0);
 
   // ---- combine the waves ----
 #pragma unroll

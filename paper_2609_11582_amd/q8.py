@@ -201,50 +201,50 @@ def okvq_rotary(rotary: RotaryParams, q, k, positions, q_out, k_out, lens=None, 
 # ---- head norms with the rotation ------------------------------------------------------------------
 
 
-def _norm_rows(q, k, q_more, k_more, names):
-    """Sizes of a call, and the rows of each kind as packed bytes: the input's, then those of q_more or k_more (tensors of the
-    input's shape and type, named by `names`)."""
+def _norm_sizes(q, k, positions):
+    """(batch, tokens, type, device, address of the positions) of a call; which of q and k is given, and how their tensors agree, is
+    checked with the rows."""
     some = q if q is not None else k
     if (not isinstance(some, torch.Tensor) or not some.is_cuda or some.dim() != 4 or some.dtype not in _ROW_TYPES
             or some.shape[3] != 128):
         raise ValueError("q, k: expected fp16 or bf16 device tensors [batch][heads][tokens][128]")
     B, _, n, _ = some.shape
-    dt, device = some.dtype, _device()
-    heads, rows = [], []
-    for kind, x, more in (("q", q, q_more), ("k", k, k_more)):
-        if any((x is None) != (y is None) for y in more):
-            raise ValueError(f"{kind}: the rows and all that belongs to them, or none of it")
-        if x is None:
-            heads.append(0)
-            rows.append((None,) * (1 + len(more)))
-            continue
-        h = x.shape[1] if isinstance(x, torch.Tensor) and x.dim() == 4 else 0
-        shape = (B, h, n, 128)
-        heads.append(h)
-        rows.append(tuple(_rows_of(y, shape, dt, name.format(kind), device) for y, name in zip((x, *more), ("{}",) + names)))
-    return B, heads, n, dt, device, rows
-
-
-def _norm_weight(w, x, name: str, device: int):
-    if (w is None) != (x is None):
-        raise ValueError(f"{name}: one for each kind of rows that is given")
-    return None if w is None else _need_rows(w, (128,), torch.float32, name, device)
-
-
-def _positions_of(positions, B, n, device):
+    device = _device()
     pos = _need(positions, 0, torch.int32, "positions", device)
     if positions.shape != (B, 3, n):
         raise ValueError(f"positions: {list(positions.shape)}, expected {[B, 3, n]}")
-    return pos
+    return B, n, some.dtype, device, pos
+
+
+def _heads_of(x, name: str, *others) -> int:
+    for y in others:
+        if (y is None) != (x is None):
+            raise ValueError(f"{name}: the rows and all that belongs to them, or none of it")
+    return 0 if x is None else x.shape[1] if isinstance(x, torch.Tensor) and x.dim() == 4 else 0
+
+
+def _norm_weight(w, name: str, device: int) -> int:
+    if not isinstance(w, torch.Tensor) or w.shape != (128,):
+        raise ValueError(f"{name}: expected 128 values")
+    return _need(w, 0, torch.float32, name, device)
 
 
 def okvq_norm_rotary(rotary: RotaryParams, q, k, q_weight, k_weight, eps, positions, q_out, k_out, lens=None, flags=0, stream=None,
                      check=True) -> int:
     """okvq_rotary of rows divided by their root mean square (of the 128 channels, with eps) and weighted: q_weight,
     k_weight fp32 [128], or None with their rows."""
-    B, (hq, hk), n, dt, device, ((rq, oq), (rk, ok)) = _norm_rows(q, k, (q_out,), (k_out,), ("{}_out",))
-    st = lib().okvq_norm_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, _norm_weight(q_weight, q, "q_weight", device),
-                                _norm_weight(k_weight, k, "k_weight", device), float(eps), _positions_of(positions, B, n, device),
+    B, n, dt, device, pos = _norm_sizes(q, k, positions)
+    hq, hk = _heads_of(q, "q", q_weight, q_out), _heads_of(k, "k", k_weight, k_out)
+    rq = oq = wq = rk = ok = wk = None
+    if q is not None:
+        shape = (B, hq, n, 128)
+        rq, oq = _rows_of(q, shape, dt, "q", device), _rows_of(q_out, shape, dt, "q_out", device)
+        wq = _norm_weight(q_weight, "q_weight", device)
+    if k is not None:
+        shape = (B, hk, n, 128)
+        rk, ok = _rows_of(k, shape, dt, "k", device), _rows_of(k_out, shape, dt, "k_out", device)
+        wk = _norm_weight(k_weight, "k_weight", device)
+    st = lib().okvq_norm_rotary(ctypes.byref(rotary), B, hq, hk, n, rq, rk, wq, wk, float(eps), pos,
                                 None if lens is None else _ints(lens, B, "lens"), oq, ok, _ROW_TYPES[dt],
                                 _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
@@ -265,13 +265,21 @@ def okvq_norm_rotary_backward(rotary: RotaryParams, q, k, q_weight, k_weight, ep
                               dk_weight, workspace, lens=None, flags=0, stream=None, check=True) -> int:
     """Gradients of okvq_norm_rotary: q_grad, k_grad of its outputs; dq, dk (rows, any strides) and dq_weight, dk_weight
     (fp32 [128], overwritten) are written."""
-    B, (hq, hk), n, dt, device, ((rq, gq, oq), (rk, gk, ok)) = _norm_rows(q, k, (q_grad, dq), (k_grad, dk), ("{}_grad", "d{}"))
-    st = lib().okvq_norm_rotary_backward(
-        ctypes.byref(rotary), B, hq, hk, n, rq, rk, _norm_weight(q_weight, q, "q_weight", device),
-        _norm_weight(k_weight, k, "k_weight", device), float(eps), _positions_of(positions, B, n, device),
-        None if lens is None else _ints(lens, B, "lens"), gq, gk, oq, ok, _norm_weight(dq_weight, q, "dq_weight", device),
-        _norm_weight(dk_weight, k, "dk_weight", device), _ROW_TYPES[dt], _need(workspace, 0, None, "workspace", device),
-        workspace.nbytes, _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
+    B, n, dt, device, pos = _norm_sizes(q, k, positions)
+    hq, hk = _heads_of(q, "q", q_weight, q_grad, dq, dq_weight), _heads_of(k, "k", k_weight, k_grad, dk, dk_weight)
+    of_q = of_k = (None,) * 5
+    if q is not None:
+        shape = (B, hq, n, 128)
+        of_q = (_rows_of(q, shape, dt, "q", device), _rows_of(q_grad, shape, dt, "q_grad", device), _rows_of(dq, shape, dt, "dq", device),
+                _norm_weight(q_weight, "q_weight", device), _norm_weight(dq_weight, "dq_weight", device))
+    if k is not None:
+        shape = (B, hk, n, 128)
+        of_k = (_rows_of(k, shape, dt, "k", device), _rows_of(k_grad, shape, dt, "k_grad", device), _rows_of(dk, shape, dt, "dk", device),
+                _norm_weight(k_weight, "k_weight", device), _norm_weight(dk_weight, "dk_weight", device))
+    st = lib().okvq_norm_rotary_backward(ctypes.byref(rotary), B, hq, hk, n, of_q[0], of_k[0], of_q[3], of_k[3], float(eps), pos,
+                                         None if lens is None else _ints(lens, B, "lens"), of_q[1], of_k[1], of_q[2], of_k[2], of_q[4],
+                                         of_k[4], _ROW_TYPES[dt], _need(workspace, 0, None, "workspace", device), workspace.nbytes,
+                                         _int(flags, "flags", 0, (1 << 32) - 1), _stream(stream))
     if check and st:
         _check(st, "okvq_norm_rotary_backward")
     return st
