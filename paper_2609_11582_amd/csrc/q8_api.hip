@@ -230,7 +230,9 @@ okvq_status attend(Q8AttendArgs& a, int span, const okvq_q8_cache* cache, int32_
   }
   Q8Plan plan;
   q8_plan(plan, d.batch, d.num_kv_heads, G, most, span == kQ8Full ? lens_host : spans, n_new_host, span);
-  const size_t need = span == kQ8Tree ? q8_tree_workspace(plan, d.num_kv_heads) : q8_workspace_bound(G, most);
+  const size_t need = span == kQ8Tree     ? q8_tree_workspace(plan, d.num_kv_heads)
+                      : span == kQ8Window ? q8_span_workspace_bound(G, most)
+                                          : q8_workspace_bound(G, most);
   if (!aligned16(workspace) || workspace_bytes < need) return OKVQ_ERR_WORKSPACE;
   const int64_t units = (int64_t)plan.ntile * d.num_kv_heads;
   if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
@@ -364,7 +366,7 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
 
 size_t okvq_q8_workspace_bytes(const okvq_q8_dims* d, int32_t max_seq_len, int32_t n_max) {
   if (check_dims(d) != OKVQ_OK || max_seq_len < 0 || n_max < 1) return 0;
-  return q8_workspace_bound(d->num_q_heads / d->num_kv_heads, n_max);
+  return q8_span_workspace_bound(d->num_q_heads / d->num_kv_heads, n_max);
 }
 
 okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,

@@ -156,7 +156,16 @@ constexpr Q8Unit q8_unit(const Q8Splits& s, const Q8Units& units, int H, int nti
 }
 
 constexpr int kFewRows = 32;  // rows of a head that always take the split kernel
-constexpr int kWideRows = 256; // and that take the wide kernel at most, where they see a window or precede a tree
+
+// Where the wide kernel's tiles are more than compute units: microseconds of its rounds against those of the kernel that would take
+// the call otherwise, from the starts and ends of a work-group and its time a token (256 work-groups at once, of the split
+// kernel 512), as measured over the calls that the plan's comment names and six more. tokens: wide tiles x tokens
+inline bool q8_wide_is_faster(int64_t rows, int64_t units16, int64_t units64, int64_t units256, double tokens) {
+  const double wide = 15.5 * units64 / 256 + 0.0071 * tokens / 256, mean = tokens / units64;
+  if (rows <= kFewRows) return wide < (4.0 + 0.0166 * mean) * units16 / 512;
+  const double u256 = units256 / 256.0;
+  return wide < 8.5 * std::max(1.0, u256) + u256 * mean / 64 * (0.8 + 1.24 * std::min<int64_t>(rows, 256) / 256);
+}
 
 // Every split takes the same number of tokens at most, the least that needs no more work-groups than fit the GPU at
 // once: a ragged batch is shared evenly (16 sequences of 8704 to 16384 tokens: 46 -> 41 us against as many splits for each).
@@ -187,6 +196,17 @@ constexpr int kWideRows = 256; // and that take the wide kernel at most, where t
 //   a place are split into such means, as far as there are records (4 heads, one token: 200 sequences of 300 tokens and one of
 //   131072 627 -> 38.5 us, 200 spread over 64 to 16384 176 -> 132). From the mean itself on, 200 of 2000 and one of 4096
 //   81.7 -> 85.7, 200 even up to 16000 354 -> 348.
+// Where rows see a window or precede a tree (span), lens are the tokens that a tile walks (q8_span), and:
+// * The wide kernel, 64 columns at a time, takes what the split kernel does not (which has up to 16 rows, and beyond what the second
+//   rule above gives it) as long as its tiles find a place at once. Its time goes with the columns rounded up to 64, the
+//   prompt kernel's with those rounded up to 256, at much the same rate: 32 rows 84 -> 50 us (16 slots of 16384 tokens x 4 heads, against
+//   the split kernel), 112 rows 30 -> 23 (4 heads x 32768 tokens, against the prompt kernel), 280 rows 54 -> 37, 320 rows x 131072 tokens
+//   154 -> 108, 448 rows 56 -> 48, 512 rows x 131072 tokens 159 -> 161. With more tiles than compute units it takes more rounds,
+//   each with a start and an end, and is taken where that pays (4 heads of 128 slots: 56 rows at 2000 tokens 113 -> 80 us, 28 rows 90 -> 64;
+//   not for 112 rows, 139 and 154, nor for 28 rows at 300 tokens, 30 and 34; prompts with windows of 1024 170 and 235).
+// * The prompt kernel's tiles of 128 columns where short windows leave compute units idle, or take more than one round of tiles of
+//   256, whose last one is seldom full: two work-groups share a compute unit and end one by one (8192 rows x 28 heads, window 1024: 896
+//   tiles 192 -> 175 us; 1024 tiles, 4 full rounds, 196 -> 194; 256 tiles, one round, 49 -> 55). Windows of 2000 and more: 5 % slower.
 // most_new: the most new rows of a slot, 1 at least.
 // Tiles of 256 columns x heads are below 2^23 a slot (checked before), so that no product here passes 64 bits.
 inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t* lens, const int32_t* n_new, int span = 0) {
@@ -194,6 +214,7 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
   const auto tiles = [&](int b, int cols) { return ((int64_t)n_new[b] * G + cols - 1) / cols; };
   int longest = 0, active = 0, fewest = most_new;
   int64_t units16 = 0, units64 = 0, units256 = 0, work16 = 0;  // tiles of all heads, and tiles x tokens
+  double tokens64 = 0;
   for (int b = 0; b < B; ++b) {
     if (n_new[b] == 0) continue;
     ++active;
@@ -202,15 +223,19 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     units16 += n;
     if (units16 <= kQ8Groups) work16 += n * lens[b];
     fewest = std::min(fewest, n_new[b]);
-    if (rows > kFewRows) {
+    if (rows > (span ? kQ8Cols : kFewRows)) {
       units64 += tiles(b, kQ8WideCols) * H;
+      tokens64 += (double)(tiles(b, kQ8WideCols) * H) * lens[b];
       units256 += tiles(b, kQ8PromptCols) * H;
     }
   }
   const int64_t launched = (rows + kQ8Cols - 1) / kQ8Cols * H * B;
-  const bool few = rows <= kFewRows || (units16 <= kQ8Groups && work16 <= 1 << 18 && launched <= 16 * kQ8Groups);
-  const bool wide = span != 0 && !few && rows <= kWideRows;
-  const bool half = rows > 128 && longest <= 2048 && units256 <= 256;
+  bool few = rows <= (span ? kQ8Cols : kFewRows) || (units16 <= kQ8Groups && work16 <= 1 << 18 && launched <= 16 * kQ8Groups);
+  const bool wide = span != 0 && !few && (units64 <= kQ8PromptGroups || q8_wide_is_faster(rows, units16, units64, units256, tokens64));
+  few = few || (rows <= kFewRows && !wide);
+  const bool half = rows > 128 && (span != 1        ? longest <= 2048 && units256 <= 256
+                                   : units256 <= 128 ? longest <= 2048
+                                                     : longest <= 1536 && units256 > 256);
   p.cols = few ? kQ8Cols : wide ? kQ8WideCols : half ? kQ8PromptCols / 2 : kQ8PromptCols;
   p.ntile = (int)((rows + p.cols - 1) / p.cols);
   p.rows = (int)std::min<int64_t>(rows, p.cols);
@@ -303,16 +328,21 @@ inline size_t q8_workspace_bound(int G, int n_max) {
   const size_t few = (size_t)kQ8Groups * kQ8Cols, many = (size_t)kQ8PromptGroups * kQ8PromptCols;
   return ((int64_t)n_max * G > kFewRows ? std::max(few, many) : few) * kQ8Record * sizeof(float);
 }
+// the same where rows see a window or precede a tree: the wide kernel takes up calls of fewer rows
+inline size_t q8_span_workspace_bound(int G, int n_max) {
+  const size_t wide = (size_t)kQ8PromptGroups * kQ8WideCols * kQ8Record * sizeof(float);
+  return (int64_t)n_max * G > kQ8Cols ? std::max(q8_workspace_bound(G, n_max), wide) : q8_workspace_bound(G, n_max);
+}
 
 // A tree's records: those of the splits, then one for each tile of each slot and head that has one split
 inline int64_t q8_split_records(const Q8Plan& p, int H) { return (int64_t)(p.splits.part[p.splits.order.split_slots] & 0xffffu) * H; }
 inline size_t q8_tree_workspace(const Q8Plan& p, int H) {
   return (q8_split_records(p, H) + (int64_t)p.splits.order.slots * H * p.ntile) * p.cols * kQ8Record * sizeof(float);
 }
-// and of every call of up to n_max rows: the tiles of 16 columns, or of up to 256 where there are more than kFewRows rows
+// and of every call of up to n_max rows: the tiles have 16 columns, 64 at most from 17 rows and 256 at most from 33 rows on
 inline size_t q8_tree_workspace_bound(int B, int H, int G, int n_max) {
-  const int64_t rows = (int64_t)n_max * G, cols = rows > kFewRows ? kQ8PromptCols : kQ8Cols;
-  return q8_workspace_bound(G, n_max) + (size_t)B * H * ((rows + cols - 1) / cols * cols) * kQ8Record * sizeof(float);
+  const int64_t rows = (int64_t)n_max * G, cols = rows > kFewRows ? kQ8PromptCols : rows > kQ8Cols ? kQ8WideCols : kQ8Cols;
+  return q8_span_workspace_bound(G, n_max) + (size_t)B * H * ((rows + cols - 1) / cols * cols) * kQ8Record * sizeof(float);
 }
 
 }  // namespace okvq

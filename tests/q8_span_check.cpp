@@ -64,8 +64,9 @@ int main() {
     q8_plan(p, B, H, G, most, spans.data(), n_new.data(), span);
     if (p.splits.order.split_slots + 1 > (int)(sizeof(p.splits.part) / 4)) fail("too many split slots", B, H, G, most);
     const int64_t single = q8_split_records(p, H), all = (int64_t)q8_tree_workspace(p, H) / sizeof(float) / ((int64_t)p.cols * kQ8Record);
+    if (q8_span_workspace_bound(G, most) > q8_span_workspace_bound(G, n_max)) fail("window's bound", B, H, G, most);
     if (q8_tree_workspace(p, H) > q8_tree_workspace_bound(B, H, G, n_max)) fail("bound", B, H, G, most);
-    if (single * p.cols > (int64_t)q8_workspace_bound(G, most) / 4 / kQ8Record) fail("split records", B, H, G, most);
+    if (single * p.cols > (int64_t)q8_span_workspace_bound(G, most) / 4 / kQ8Record) fail("split records", B, H, G, most);
     // every slot, head, tile and split is met by one work-group
     std::set<int64_t> met, done;
     const auto meet = [&](int place, int x, int h, int tile) {
