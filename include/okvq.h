@@ -508,7 +508,7 @@ okvq_status okvq_norm_rotary(const okvq_rotary_params* params, int32_t batch, in
                              const float* k_weight, float eps, const int32_t* positions, const int32_t* lens_host,
                              const okvq_rows* q_out, const okvq_rows* k_out, int32_t dtype, uint32_t flags, void* stream);
 
-/* Device workspace bytes of okvq_norm_rotary_backward (0 for invalid arguments; 1 MiB whatever the call). No initial
+/* Device workspace bytes of okvq_norm_rotary_backward (0 for invalid arguments; 768 KiB whatever the call). No initial
  * contents; calls that may overlap, captured graphs among them, need one each. */
 size_t okvq_norm_rotary_workspace_bytes(int32_t batch, int32_t n_tokens);
 

@@ -11,7 +11,8 @@
 //
 // The weights' gradient: a lane adds up its 16 channels over all the rows that it meets, a work-group its lanes, and
 // a second launch the work-groups, all in a fixed order: the same inputs give the same bits. So the backward's
-// work-groups are few (kParts) and take one tile after the other.
+// work-groups are few (kNormParts: one round of the GPU; 8192 tokens x 32 heads 38.5 us, with 1024 40.4, 512 37.6, but 4 sequences of
+// 2999 x 18 heads 29.7, 29.7 and 30.3) and take one tile after the other.
 #include <algorithm>
 
 #include "q8.hpp"

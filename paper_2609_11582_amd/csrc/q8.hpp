@@ -31,7 +31,7 @@ struct NormRotaryArgs {
   okvq_rows q_grad, k_grad; // backward: gradients of what the forward pass wrote
   float* parts;             // backward: [n][2][128] sums of work-groups
 };
-constexpr int kNormParts = 1024;  // work-groups of a backward pass at most (four to a compute unit), or its launches
+constexpr int kNormParts = 768;   // work-groups of a backward pass at most: three to a compute unit, what their registers allow
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, hipStream_t s);
 int norm_rotary_parts(int max_len, int nb, int launches);  // work-groups of one of the launches of a backward pass
 hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s);

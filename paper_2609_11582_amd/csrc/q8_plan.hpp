@@ -181,7 +181,10 @@ inline bool q8_wide_is_faster(int64_t rows, int64_t units16, int64_t units64, in
 //   others a work-group each: up to 8192 of them it is faster all the same (100 rows beside 15 single tokens of 4 heads 14.5 us
 //   against 25.9, 250 rows beside 63 of 1 head 16.7 against 26.0), with 11000 no longer (one prompt of 100 in 64 slots 16.1 against 10.9).
 // * One split up to 4 rounds of a block for each wave, which saves the merge launch (on the device; the host has one launch
-//   less to make too): 300 tokens 8.4 -> 6.2 us, 512 8.5 -> 7.0, 1024 8.6 -> 9.2.
+//   less to make too): 300 tokens 8.4 -> 6.2 us, 512 8.5 -> 7.0, 1024 8.6 -> 9.2. Windows, whose walk waits for the length: up to 7 (4 heads,
+//   windows of 1024: 1 slot 12.3 -> 9.6 us, 16 slots 12.8 -> 9.8, 64 slots 20.5 -> 14.1; of 1500 12.0 -> 11.3; of 1900, 8 rounds, 12.0 ->
+//   13.1). Trees, which
+//   are merged in any case, up to 3: 300 tokens 13.6 -> 11.8, 1000 (4 rounds) 13.7 -> 14.0.
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 11.2 us, with 128 splits 13.1),
 //   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 18.3 -> 14.4 us).
 // * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
@@ -266,7 +269,8 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     if (fits(mid)) hi = mid;
     else lo = mid + 1;
   }
-  if (few && longest <= 4 * round) hi = 4;
+  const int64_t alone = span == 1 ? 7 : span == 2 ? 3 : 4;
+  if (few && longest <= alone * round) hi = alone;
   const bool idle = units * 64 < 256 && longest > 64 * 4 * round;
   const int64_t cap = idle ? kQ8MaxSplits : 64;
   Q8Splits& s = p.splits;

@@ -60,7 +60,7 @@ def test_backward_refused():
 
 
 def test_workspace():
-    assert WS == 1 << 20 and q8.okvq_norm_rotary_workspace_bytes(65535, 1 << 20) == WS
+    assert WS == 768 << 10 and q8.okvq_norm_rotary_workspace_bytes(65535, 1 << 20) == WS
     assert q8.okvq_norm_rotary_workspace_bytes(0, 4) == 0 and q8.okvq_norm_rotary_workspace_bytes(1, -1) == 0
     with pytest.raises(ValueError):
         q8.okvq_norm_rotary_workspace_bytes(1 << 32, 4)
