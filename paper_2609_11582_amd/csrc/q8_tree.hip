@@ -35,15 +35,12 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_tree_merge(Q8Attend
   const int h = blockIdx.y / ntile, tile = blockIdx.y - h * ntile;
   const Q8Part mine = q8_part(order, w, next, place, 0, tile);
   const int b = order.flags & kQ8Reordered ? q8_slot_at(p.splits, place) : place;
-  const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
   const int tid = threadIdx.x, lane = tid & 31, team = tid >> 5, grp = team % kGroups, cc = blockIdx.x * kCols + team / kGroups;
   const int r = tile * cols + min(cc, cols - 1), i = r / p.G, hq = h * p.G + (r - i * p.G);
-  if ((tile * cols + (int)blockIdx.x * kCols) / p.G >= n) return;  // the whole work-group
-  const bool live = cc < cols && i < n;
-  if (kGroups == 1 && !live) return;
-  const int row = min(i, n - 1);  // of teams without one: any
+  const int row = min(i, p.n_max - 1);  // of teams without one: any
 
-  // the splits' sums, a group every kGroups-th, and their statistics, a lane every 32nd
+  // the splits' sums, a group every kGroups-th, and their statistics, a lane every 32nd. These and the rows below go out before the
+  // count says whether they are needed (every column of a tile has its place in a record)
   const int nsplit = mine.nsplit, recf = cols * kQ8Record;
   const int64_t first = mine.records ? (int64_t)(mine.first * p.c.H + h * mine.records + tile * nsplit)
                                      : p.single + ((int64_t)b * p.c.H + h) * ntile + tile;
@@ -67,7 +64,12 @@ __global__ __launch_bounds__(32 * kGroups * kCols) void k_q8_tree_merge(Q8Attend
   // the group's drafts: those of its residue modulo kGroups
   const uint32_t* mask = p.visible + ((int64_t)b * p.n_max + row) * p.words;
   uint32_t word = mask[0];
-  const uint2 qr = *reinterpret_cast<const uint2*>(p.q + (((int64_t)b * p.c.Hq + hq) * p.n_max + row) * kD + 4 * lane);
+  const uint2 qr = *reinterpret_cast<const uint2*>(p.q + (((int64_t)b * p.c.Hq + min(hq, p.c.Hq - 1)) * p.n_max + row) * kD + 4 * lane);
+  __asm__ volatile("" ::: "memory");
+  const int n = min(max(uniform_load(p.n_new + b), 0), p.n_max);
+  if ((tile * cols + (int)blockIdx.x * kCols) / p.G >= n) return;  // the whole work-group
+  const bool live = cc < cols && i < n;
+  if (kGroups == 1 && !live) return;
   const float q0 = row_lo<kBf16>(qr.x), q1 = row_hi<kBf16>(qr.x), q2 = row_lo<kBf16>(qr.y), q3 = row_hi<kBf16>(qr.y);
   const int64_t rows = ((int64_t)b * p.c.H + h) * p.n_max * kD + 4 * lane;
   uint32_t mine_of_word = 0;

@@ -114,5 +114,26 @@ int main() {
       }
     if (!met.empty()) fail("left over", B, H, G, most);
   }
+  // the shapes that tests on the GPU mean for the wide kernel
+  const auto cols = [&](std::vector<int32_t> lens, std::vector<int32_t> n, int H, int G, int window, int sinks, int span) {
+    std::vector<int32_t> spans;
+    for (size_t b = 0; b < lens.size(); ++b) spans.push_back(q8_span(lens[b], n[b], G, window, sinks));
+    Q8Plan p;
+    q8_plan(p, (int)lens.size(), H, G, *std::max_element(n.begin(), n.end()), spans.data(), n.data(), span);
+    return p.cols;
+  };
+  std::vector<int32_t> lens, n, l16;
+  for (int b = 0; b < 40; ++b) {
+    const int32_t some[] = {0, 1, 31, 32, 33, 64, 65, 100, 500, 1003};
+    lens.push_back(some[b * 7 % 10]);
+    n.push_back(b % 5 == 0 ? b % 16 : 16);
+  }
+  for (int b = 0; b < 16; ++b) l16.push_back(4096 - 37 * b);
+  if (cols({20011}, {16}, 1, 16, INT_MAX, 0, 2) != kQ8WideCols || cols({30000}, {16}, 1, 16, 17000, 33, 2) != kQ8WideCols ||
+      cols({30000}, {16}, 1, 16, 16900, 0, 2) != kQ8WideCols || cols({20000}, {20}, 1, 16, 15000, 70, 1) != kQ8WideCols ||
+      cols(lens, n, 2, 8, INT_MAX, 0, 2) != kQ8WideCols || cols(lens, n, 2, 8, 50, 3, 2) != kQ8WideCols || cols(lens, n, 2, 8, 90, 40, 1) != kQ8WideCols ||
+      cols(std::vector<int32_t>(40, 300), std::vector<int32_t>(40, 16), 2, 8, INT_MAX, 0, 2) != kQ8WideCols ||
+      cols(l16, std::vector<int32_t>(16, 3), 4, 7, INT_MAX, 0, 2) != kQ8WideCols || cols({20000}, {128}, 1, 2, INT_MAX, 0, 2) != kQ8WideCols)
+    fail("not wide", 0, 0, 0, 0);
   std::printf("ok\n");
 }

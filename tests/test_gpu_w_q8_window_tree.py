@@ -181,8 +181,9 @@ def _tree(c, lens, q, k, v, visible, n_draft, window=0, sinks=0, sm=SM, layer=0,
     return out
 
 
-def _check_tree(c, out, lens, q, kd, vd, visible, n_draft, fmt, dtype, tag, window=0, sinks=0, sm=SM, layer=0, fill=9.0, scale=1.0):
-    """scale: what values and outputs are divided by before they are compared"""
+def _check_tree(c, out, lens, q, kd, vd, visible, n_draft, fmt, dtype, tag, window=0, sinks=0, sm=SM, layer=0, fill=9.0, scale=1.0,
+                rows=None):
+    """scale: what values and outputs are divided by before they are compared; rows: those compared, all if None"""
     a, got = _numpy(c), _np(out)
     B, Hq, n, _ = q.shape
     H = c.dims.num_kv_heads
@@ -192,15 +193,16 @@ def _check_tree(c, out, lens, q, kd, vd, visible, n_draft, fmt, dtype, tag, wind
         assert np.all(got[b, :, m:] == fill), f"{tag}: rows behind the last draft were written"
         if not m:
             continue
-        seen = oq.tree_seen(lens[b], visible[b], m, window, sinks)
+        pick = np.arange(m) if rows is None else np.unique(np.clip(rows, 0, m - 1))
+        seen = oq.tree_seen(lens[b], visible[b], m, window, sinks)[pick]
         for h in range(H):
             k, v = oq.read_sequence(a, layer, b, h, lens[b], fmt)
             k, v = np.concatenate([k, _np(kd[b, h, :m])]), np.concatenate([v, _np(vd[b, h, :m])]) / scale
             k, v = np.where(seen.any(0)[:, None], k, 0), np.where(seen.any(0)[:, None], v, 0)
             for j in range(h * G, (h + 1) * G):
-                ref, bound = oq.attention_where(_np(q[b, j, :m]), k, v, seen, sm, HALF[dtype])
-                assert np.all(got[b, j, :m][~seen.any(1)] == 0), f"{tag}: a row that sees nothing yields zeros"
-                worst = max(worst, _worst(got[b, j, :m] / scale, ref, bound))
+                ref, bound = oq.attention_where(_np(q[b, j, pick]), k, v, seen, sm, HALF[dtype])
+                assert np.all(got[b, j, pick][~seen.any(1)] == 0), f"{tag}: a row that sees nothing yields zeros"
+                worst = max(worst, _worst(got[b, j, pick] / scale, ref, bound))
     _say(f"{tag}: worst err / bound {worst:.3f}")
     assert worst <= 1
 
@@ -345,6 +347,114 @@ def test_many_slots():
     new = [min(1, L) for L in lens]
     out = _window(c, lens, q[:, :, :1].contiguous(), new, 30, 4)
     _check_window(c, out, lens, q[:, :, :1].contiguous(), new, 30, 4, "int8", "fp16", "300 slots, a window")
+
+
+# ---- the wide kernel: shapes that take it (q8_span_check.cpp holds the plan to that) --------------
+
+
+@pytest.mark.parametrize("fmt, dtype, window, sinks", [("int8", "fp16", 0, 0), ("e4m3", "bf16", 0, 0), ("int8", "bf16", 17000, 33),
+                                                       ("e4m3", "fp16", 16900, 0)])
+def test_wide_tree_over_a_long_sequence(fmt, dtype, window, sinks):
+    L, n, Hq = 20011 if not window else 30000, 16, 16
+    c = _filled(1, 1, Hq, [L], 64, fmt, dtype, 121, drift=0.02)
+    q, k, v = _drafts(122, 1, 1, Hq, n, dtype)
+    visible = _masks([_parents(np.random.default_rng(123), n, "any")], n)
+    out = _tree(c, [L], q, k, v, visible, [n], window, sinks)
+    _check_tree(c, out, [L], q, k, v, visible, [n], fmt, dtype, f"wide tree {fmt} {dtype} {window}+{sinks}", window, sinks,
+                rows=np.array([0, 3, 4, 15]))
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+def test_wide_window_of_a_chunk(fmt, dtype):
+    L, n, Hq, window, sinks = 20000, 20, 16, 15000, 70
+    c = _filled(1, 1, Hq, [L], 128, fmt, dtype, 124, drift=0.02)
+    q = _rows(125, 1, Hq, n + 3, 128, dtype=dtype, scale=1.5)
+    out = _window(c, [L], q, [n], window, sinks)
+    _check_window(c, out, [L], q, [n], window, sinks, fmt, dtype, f"wide window {fmt} {dtype}", rows=np.array([0, 3, 4, 19]))
+
+
+def _many(host=False):
+    """40 slots, most with 16 drafts, of many lengths; host: what a captured call's host arrays may say instead"""
+    lens = [(0, 1, 31, 32, 33, 64, 65, 100, 500, 1003)[(b * 7) % 10] for b in range(40)]
+    n = [b % 16 if b % 5 == 0 else 16 for b in range(40)]
+    return ([300] * 40, [16] * 40) if host else (lens, n)
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("window, sinks, host", [(0, 0, False), (50, 3, False), (0, 0, True)])
+def test_wide_tree_of_many_slots(fmt, dtype, window, sinks, host):
+    (lens, n_draft), n = _many(), 16
+    host_lens, host_n = _many(host)
+    c = _filled(40, 2, 16, lens, 32, fmt, dtype, 126)
+    q, k, v = _drafts(127, 40, 2, 16, n, dtype)
+    visible = _masks([_parents(np.random.default_rng(b), m, "any") for b, m in enumerate(n_draft)], n)
+    out = _tree(c, host_lens, q, k, v, visible, host_n, window, sinks, n_dev=_i32(n_draft))
+    _check_tree(c, out, lens, q, k, v, visible, n_draft, fmt, dtype, f"wide tree of 40 slots {fmt} {dtype} {window}+{sinks}", window, sinks,
+                rows=np.arange(0, 16, 3))
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+def test_wide_window_of_many_slots(fmt, dtype):
+    (lens, new), n = _many(), 16
+    c = _filled(40, 2, 16, lens, 32, fmt, dtype, 128)
+    q = _rows(129, 40, 16, n, 128, dtype=dtype, scale=1.5)
+    out = _window(c, lens, q, new, 90, 40)
+    _check_window(c, out, lens, q, new, 90, 40, fmt, dtype, f"wide window of 40 slots {fmt} {dtype}",
+                  rows=np.arange(0, 16, 3))
+
+
+def test_wide_of_few_rows():
+    lens, n = [4096 - 37 * b for b in range(16)], 3
+    c = _filled(16, 4, 28, lens, 64, "int8", "fp16", 130)
+    q, k, v = _drafts(131, 16, 4, 28, n, "fp16")
+    visible = _masks([[-1, 0, 0]] * 16, n)
+    out = _tree(c, lens, q, k, v, visible, [n] * 16)
+    _check_tree(c, out, lens, q, k, v, visible, [n] * 16, "int8", "fp16", "wide tree of 21 rows")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("case", range(4))
+def test_wide_dominant_tokens_and_uneven_values(fmt, case):
+    """A flat background with tokens 10 to 30 log2 units above it, growing and falling along the sequence, whose values
+    are small where attention is large (and the other way round); blocks of zero values."""
+    import torch
+    L, n = 20000, 128
+    c = _new(1, 1, 2, [L], 64, fmt)
+    g = torch.Generator().manual_seed(140 + case)
+    k, v = 0.01 * torch.randn(1, 1, L, 128, generator=g), 0.01 * torch.randn(1, 1, L, 128, generator=g) + 1.0
+    at = torch.arange(0, L, 512)
+    k[0, 0, at, 0] = torch.linspace(10, 30, len(at)) if case % 2 else torch.linspace(30, 10, len(at))
+    v[0, 0] *= torch.where(torch.arange(L) % 512 < 32, 2.0 ** -9 if case < 2 else 2.0 ** 9, 1.0)[:, None]
+    v[0, 0, 640:704] = 0
+    k, v = k.half(), v.half()
+    _append(c, 0, k, v, [0], [L])
+    q = torch.zeros(1, 2, n, 128)
+    q[:, :, :, 0] = math.log(2.0) / SM  # scores are the first channel, in log2 units
+    q[:, 1] *= 0.3
+    kd, vd = 0.01 * torch.randn(1, 1, n, 128, generator=g), torch.randn(1, 1, n, 128, generator=g)
+    kd[0, 0, ::3, 0] = 29
+    q, kd, vd = q.half(), kd.half(), vd.half()
+    visible = _masks([[-1] * n], n)
+    out = _tree(c, [L], q, kd, vd, visible, [n])
+    _check_tree(c, out, [L], q, kd, vd, visible, [n], fmt, "fp16", f"wide dominant {fmt} case {case}", rows=np.array([0, 1, 31, 32, 127]))
+
+
+@pytest.mark.parametrize("sm", [0.0, -0.05, 2.0])
+def test_wide_softmax_scales_and_subnormal_values(sm):
+    """Values of scales below 2^-126 count as nothing beside others; negative and zero scales."""
+    import torch
+    L, n, Hq = 20000, 16, 16
+    c = _filled(1, 1, Hq, [L], 64, "int8", "bf16", 150, drift=0.02)
+    k, v = _rows(151, 1, 1, 64, 128, dtype="bf16"), (_rows(152, 1, 1, 64, 128).double() * 1e-38).to(torch.bfloat16)
+    c["seq_lens"].copy_(_i32([L]))
+    page = int(c["block_table"][0, 3])
+    code, _ = oq.quantize_block(v[0, 0, :32].float().numpy(), "int8")
+    c["v_codes"][0, page, 0, 0] = torch.from_numpy(oq.pack_values(code)).cuda()
+    c["v_scale"][0, page, 0, 0] = 2.0 ** -130
+    q, kd, vd = _drafts(153, 1, 1, Hq, n, "bf16")
+    visible = _masks([_parents(np.random.default_rng(154), n, "any")], n)
+    out = _tree(c, [L], q, kd, vd, visible, [n], sm=sm)
+    _check_tree(c, out, [L], q, kd, vd, visible, [n], "int8", "bf16", f"wide scale {sm}", sm=sm, rows=np.array([0, 3, 4, 15]))
 
 
 # ---- as they are used ----------------------------------------------------------------------------
