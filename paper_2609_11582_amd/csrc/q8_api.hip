@@ -225,7 +225,9 @@ okvq_status attend(Q8AttendArgs& a, int span, const okvq_q8_cache* cache, int32_
   if (!launchable(((int64_t)most * G + kQ8PromptCols - 1) / kQ8PromptCols * d.num_kv_heads, 512)) return OKVQ_ERR_UNSUPPORTED;
   int32_t spans[kQ8MaxBatch];
   if (span != kQ8Full) {
+    // what reaches past any sequence is cut, so that differences to it stay inside 32 bits
     a.sinks = std::min(a.sinks, capacity(d));
+    if (a.window != INT32_MAX || span == kQ8Window) a.window = std::min(a.window, capacity(d) + OKVQ_Q8_MAX_DRAFTS);
     for (int b = 0; b < d.batch; ++b) spans[b] = q8_span(lens_host[b], n_new_host[b], G, a.window, a.sinks);
   }
   Q8Plan plan;
@@ -238,7 +240,7 @@ okvq_status attend(Q8AttendArgs& a, int span, const okvq_q8_cache* cache, int32_
   if (!launchable(plan.splits.order.most * units * q8_layers(plan), 512) ||
       (plan.splits.order.most > 1 && (!launchable(units * plan.splits.order.split_slots * 32, 256) || units > 65535)) ||
       (plan.cols == kQ8WideCols && !launchable(q8_wide_groups(plan, d.num_kv_heads), 512)) ||
-      (span == kQ8Tree && (!launchable(units * d.batch * plan.rows, 512) || units > 65535)))
+      (span == kQ8Tree && (!launchable(q8_tree_merge_groups(plan, d.num_kv_heads), 512) || units > 65535)))
     return OKVQ_ERR_UNSUPPORTED;
   a.c = view(cache, layer);
   a.q = q;

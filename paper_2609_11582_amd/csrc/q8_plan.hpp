@@ -338,6 +338,23 @@ inline size_t q8_span_workspace_bound(int G, int n_max) {
   return (int64_t)n_max * G > kQ8Cols ? std::max(q8_workspace_bound(G, n_max), wide) : q8_workspace_bound(G, n_max);
 }
 
+// A tree's merge: groups of 32 lanes for a column, 8 splits each at most, and columns of a work-group
+struct Q8TreeMerge {
+  int groups, cols;
+};
+inline Q8TreeMerge q8_tree_merge(const Q8Plan& p) {
+  const int most = p.splits.order.most;
+  if (most > 64) return {16, 1};
+  if (most > 32) return {8, 1};
+  if (most > 16) return {4, 2};
+  if (most > 8) return {2, 4};
+  return {1, 8};
+}
+inline int64_t q8_tree_merge_groups(const Q8Plan& p, int H) {  // work-groups
+  const int cols = q8_tree_merge(p).cols;
+  return (int64_t)((p.rows + cols - 1) / cols) * H * p.ntile * p.splits.order.slots;
+}
+
 // A tree's records: those of the splits, then one for each tile of each slot and head that has one split
 inline int64_t q8_split_records(const Q8Plan& p, int H) { return (int64_t)(p.splits.part[p.splits.order.split_slots] & 0xffffu) * H; }
 inline size_t q8_tree_workspace(const Q8Plan& p, int H) {

@@ -7,9 +7,9 @@
 // largest size stay finite).
 //
 // Bound: latency. A column's splits and drafts are dealt to kGroups groups of 32 lanes (4 channels a lane), drafts by their number,
-// so that a group meets few of them, four at a time; the splits' statistics and sums are loaded first and used last.
-// With few splits a group takes a column alone, 8 columns a work-group (8 slots of up to 175 columns, 4 splits at most: 16.8 us with 8
-// groups a column).
+// so that a group meets few of them, four at a time; the splits' statistics and sums are loaded first and used last. 112 columns x 4
+// heads, 32 splits 4.8 us. With few splits a group takes a column alone, 8 columns a work-group (8 slots of up to 175 columns x 4 heads,
+// 4 splits: 6.9 us, with 8 groups a column 16.8).
 #include "q8_mfma.hpp"
 
 namespace okvq {
@@ -178,12 +178,13 @@ void merge(const Q8AttendArgs& a, const Q8Plan& p, bool bf16, hipStream_t s) {
 
 hipError_t launch_q8_tree_merge(const Q8AttendArgs& a, const Q8Plan& p, int dtype, hipStream_t s) {
   static_assert(kQ8MaxSplits == 16 * 8, "a group takes 8 splits at most");
-  const int most = p.splits.order.most;
-  if (most > 64) merge<16, 1>(a, p, dtype == OKVQ_BF16, s);
-  else if (most > 32) merge<8, 1>(a, p, dtype == OKVQ_BF16, s);
-  else if (most > 16) merge<4, 2>(a, p, dtype == OKVQ_BF16, s);
-  else if (most > 8) merge<2, 4>(a, p, dtype == OKVQ_BF16, s);
-  else merge<1, 8>(a, p, dtype == OKVQ_BF16, s);
+  switch (q8_tree_merge(p).groups) {
+    case 16: merge<16, 1>(a, p, dtype == OKVQ_BF16, s); break;
+    case 8: merge<8, 1>(a, p, dtype == OKVQ_BF16, s); break;
+    case 4: merge<4, 2>(a, p, dtype == OKVQ_BF16, s); break;
+    case 2: merge<2, 4>(a, p, dtype == OKVQ_BF16, s); break;
+    default: merge<1, 8>(a, p, dtype == OKVQ_BF16, s);
+  }
   return hipGetLastError();
 }
 

@@ -135,5 +135,12 @@ int main() {
       cols(std::vector<int32_t>(40, 300), std::vector<int32_t>(40, 16), 2, 8, INT_MAX, 0, 2) != kQ8WideCols ||
       cols(l16, std::vector<int32_t>(16, 3), 4, 7, INT_MAX, 0, 2) != kQ8WideCols || cols({20000}, {128}, 1, 2, INT_MAX, 0, 2) != kQ8WideCols)
     fail("not wide", 0, 0, 0, 0);
+  // and for the prompt kernel's tiles of 128 and 256 columns
+  if (cols({900}, {600}, 4, 7, 130, 40, 1) != 128 || cols({1200}, {1200}, 4, 7, 333, 5, 1) != 256 || cols({2500}, {2500}, 4, 7, 100, 65, 1) != 128 ||
+      cols({3000}, {1200}, 4, 7, 1, 0, 1) != 256 || cols({700}, {600}, 4, 7, 1 << 30, 0, 1) != 128)
+    fail("prompt", 0, 0, 0, 0);
+  std::vector<int32_t> l64, n64;
+  for (int b = 0; b < 16; ++b) l64.push_back(1500 - 90 * b), n64.push_back(b == 5 ? 0 : 64 - b);
+  if (cols(l64, n64, 4, 7, INT_MAX, 0, 2) < 128 || cols(l64, n64, 4, 7, 300, 33, 2) < 128) fail("prompt of a tree", cols(l64, n64, 4, 7, INT_MAX, 0, 2), 0, 0, 0);
   std::printf("ok\n");
 }

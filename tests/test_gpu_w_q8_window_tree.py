@@ -457,6 +457,49 @@ def test_wide_softmax_scales_and_subnormal_values(sm):
     _check_tree(c, out, [L], q, kd, vd, visible, [n], "int8", "bf16", f"wide scale {sm}", sm=sm, rows=np.array([0, 3, 4, 15]))
 
 
+# ---- the prompt kernel, whole and half tiles, split and not (q8_span_check.cpp again) ------------
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("n, L, window, sinks", [(600, 900, 130, 40), (1200, 1200, 333, 5), (2500, 2500, 100, 65), (1200, 3000, 1, 0), (600, 700, 1 << 30, 0)])
+def test_window_of_prompts(fmt, dtype, n, L, window, sinks):
+    c = _filled(1, 4, 28, [L], 64, fmt, dtype, 161)
+    q = _rows(162, 1, 28, n, 128, dtype=dtype, scale=1.5)
+    out = _window(c, [L], q, [n], window, sinks)
+    rows = np.array([0, 1, 8, 9, 17, 18, 19, 35, 36, 37, 63, 64, 100, 300, 301, 302, 500, n - 40, n - 2, n - 1])
+    _check_window(c, out, [L], q, [n], window, sinks, fmt, dtype, f"window prompt {fmt} {dtype} {n} of {L} {window}+{sinks}", rows=rows)
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("window, sinks", [(0, 0), (300, 33)])
+def test_prompt_kernel_for_trees(fmt, dtype, window, sinks):
+    """16 slots of 448 columns: tiles of 256 (of 128 with the window), two splits each, one without drafts."""
+    lens, n_draft, n = [1500 - 90 * b for b in range(16)], [0 if b == 5 else 64 - b for b in range(16)], 64
+    c = _filled(16, 4, 28, lens, 64, fmt, dtype, 163)
+    q, k, v = _drafts(164, 16, 4, 28, n, dtype)
+    visible = _masks([_parents(np.random.default_rng(b), m, "any") for b, m in enumerate(n_draft)], n)
+    out = _tree(c, lens, q, k, v, visible, n_draft, window, sinks)
+    _check_tree(c, out, lens, q, k, v, visible, n_draft, fmt, dtype, f"prompt kernel's tree {fmt} {dtype} {window}+{sinks}", window, sinks,
+                rows=np.array([0, 9, 36, 37, 63]))
+
+
+def test_windows_past_any_sequence():
+    """The largest window and sinks, rows before the first token: what reaches past a sequence is everything."""
+    import torch
+    lens, new = [5, 300, 0], [40, 40, 40]
+    c = _filled(3, 1, 7, lens, 64, "int8", "fp16", 165)
+    q = _rows(166, 3, 7, 40, 128)
+    big = (1 << 31) - 1
+    out = _window(c, lens, q, new, big, big)
+    _check_window(c, out, lens, q, new, 1 << 40, 0, "int8", "fp16", "largest window")
+    qd, k, v = _drafts(167, 3, 1, 7, 9, "fp16")
+    visible = _masks([_parents(np.random.default_rng(4), 9, "any")] * 3, 9)
+    a = _tree(c, lens, qd, k, v, visible, [9] * 3, big, 0)
+    b = _tree(c, lens, qd, k, v, visible, [9] * 3, 1 << 27, big)
+    assert torch.equal(a, b)
+    _check_tree(c, a, lens, qd, k, v, visible, [9] * 3, "int8", "fp16", "largest window of a tree")
+
+
 # ---- as they are used ----------------------------------------------------------------------------
 
 
