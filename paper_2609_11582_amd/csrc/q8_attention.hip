@@ -19,6 +19,9 @@
 //    reference, the maximum of s_t + log2 v_scale. Both references move only when a maximum passes them by 2^8,
 //    so w < 2^15 keeps full precision down to 2^-21 of the largest product, whatever the blocks' scales are; the
 //    sum of p_t stays in fp32, unrounded.
+// Where rows see a window, or precede a tree (kSpan), a wave walks those blocks of its residue that some row of the tile sees, and masks
+// their tokens row by row; a tree's part always leaves records, which q8_tree.hip joins with the drafts. One token's window of
+// 1024 behind 4 sinks: 4 heads 9.6 us, 16 slots of them 9.8, one launch each (by then two blocks a wave: latency).
 // Bound: memory in large calls (131072 tokens x 4 heads 25.4 us, 5.3 TB/s), latency in small ones (32768 tokens 9.0 us: 2
 // blocks a wave; 12.0 with the merge). 4 or 16 waves in place of 8 were 16 and 10 % slower on the build that took 13.4.
 #include <algorithm>

@@ -12,6 +12,11 @@
 //    consecutive bytes of a value block).
 //  * The weights are formed in one fused step as 2^(dot * scale + c), c = log2 v_scale + 7 - M; their sum, divided
 //    by the block's factor, is the block's share of the softmax sum.
+//  * Where rows see a window, or precede a tree (kSpan), the walk is over the blocks that some row of the work-group sees: a wave's
+//    products stop at the last tile that its own rows see, and it goes on bringing tiles for the others in a loop of its own (a
+//    branch around the products in one loop costs 60 to 160 spilled registers: 410 us in place of 190). 8192 rows
+//    x 28 heads with windows of 1024: 175 us, 0.64 PFLOP/s of what the rows see (1024 + 128 / 7 + 63 tokens are computed for each),
+//    with 2.0 us a pass of 64 tokens, 5.8 before the first and 2.4 after the last of a work-group's 19.
 // Bound: issue and power together. 512 rows against 4 x 65536 tokens run at 1.0 PFLOP/s (a large bf16 product of the
 // library at 1.2). Under the counters (1184 us, 1.88 GHz) the matrix cores are busy 47 % and the vector units 55 % of the SIMD
 // cycles, the LDS 31 %.

@@ -1,4 +1,4 @@
-"""Binding of the rotary positions and of the paged 8-bit cache of libokvq.so (include/okvq.h): argument
+"""Binding of the rotary positions, of the head norms and of the paged 8-bit cache of libokvq.so (include/okvq.h): argument
 marshalling and size checks only, as in ``okvq``. Tensors have to be on the current device and of the stated
 type; the stream is torch's current one unless one is given."""
 

@@ -38,7 +38,7 @@ BAD = [dict(par=None), dict(batch=0), dict(batch=65536), dict(n=-1), dict(pos=OF
        dict(lens=(4, 4), qo=rows(t=64)), dict(lens=None, ko=rows(b=0)), dict(lens=(4, 4), qo=rows(h=128, t=128))]
 
 
-@pytest.mark.parametrize("kw", BAD, ids=str)
+@pytest.mark.parametrize("kw", BAD, ids=[f"{i}-{'-'.join(kw)}" for i, kw in enumerate(BAD)])
 @pytest.mark.parametrize("call", [forward, backward])
 def test_refused(call, kw):
     assert call(**kw) == -1
