@@ -518,7 +518,7 @@ size_t okvq_norm_rotary_workspace_bytes(int32_t batch, int32_t n_tokens);
  *   q_grad, k_grad  device rows: gradients of q_out and k_out
  *   dq, dk     device rows, as the outputs of okvq_rotary; one may be its own gradient or input with the same strides (in
  *              place) and may not overlap a row that is read otherwise. Rows t >= lens_host[b] are left as they were
- *   dq_weight, dk_weight  device fp32 [128], overwritten with the sums over all rows (zero where there are none), in an order
+ *   dq_weight, dk_weight  device fp32 [128], one each, overwritten with the sums over all rows (zero where there are none), in an order
  *              that depends on the sizes alone: the same inputs give the same bits
  *   workspace  device, 16-byte aligned, okvq_norm_rotary_workspace_bytes(batch, n_tokens) bytes */
 okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,

@@ -312,7 +312,7 @@ okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t 
                                lens_host, dtype, flags, OKVQ_ROTARY_ADJACENT);
   if (st == OKVQ_OK) st = norm_args(a, q_weight, k_weight, eps);
   if (st != OKVQ_OK) return st;
-  if ((q && !aligned16(dq_weight)) || (k && !aligned16(dk_weight))) return OKVQ_ERR_INVALID_ARGUMENT;
+  if ((q && !aligned16(dq_weight)) || (k && !aligned16(dk_weight)) || (q && k && dq_weight == dk_weight)) return OKVQ_ERR_INVALID_ARGUMENT;
   if (!aligned16(workspace) || workspace_bytes < okvq_norm_rotary_workspace_bytes(batch, n_tokens)) return OKVQ_ERR_WORKSPACE;
   a.q_grad = q ? *q_grad : okvq_rows{};
   a.k_grad = k ? *k_grad : okvq_rows{};

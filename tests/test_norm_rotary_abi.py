@@ -25,7 +25,7 @@ def forward(par=ctypes.byref(PAR), batch=2, hq=4, hk=4, n=4, q=rows(), k=rows(),
 
 
 def backward(par=ctypes.byref(PAR), batch=2, hq=4, hk=4, n=4, q=rows(), k=rows(), qw=FAKE, kw=FAKE, eps=1e-6, pos=FAKE, lens=(9, 9),
-             qo=rows(), ko=rows(), dtype=0, flags=0, gq=rows(), gk=rows(), dqw=FAKE, dkw=FAKE, ws=FAKE, nbytes=WS):
+             qo=rows(), ko=rows(), dtype=0, flags=0, gq=rows(), gk=rows(), dqw=FAKE, dkw=ctypes.c_void_p(8192), ws=FAKE, nbytes=WS):
     lens = None if lens is None else (ctypes.c_int32 * 2)(*lens)
     return q8.lib().okvq_norm_rotary_backward(par, batch, hq, hk, n, q, k, qw, kw, ctypes.c_float(eps), pos, lens, gq, gk, qo, ko, dqw,
                                               dkw, dtype, ws, nbytes, flags, None)
@@ -52,7 +52,7 @@ def test_accepted_without_rows():
 
 
 def test_backward_refused():
-    for kw in (dict(gq=None), dict(gk=None), dict(gq=rows(4104)), dict(gk=rows(t=4)), dict(dqw=None), dict(dkw=OFF)):
+    for kw in (dict(gq=None), dict(gk=None), dict(gq=rows(4104)), dict(gk=rows(t=4)), dict(dqw=None), dict(dkw=OFF), dict(dkw=FAKE)):
         assert backward(**dict(lens=(0, 0)) | kw) == -1
     assert backward(lens=(0, 0), k=None, ko=None, kw=None) == -1           # a gradient without its rows
     for kw in (dict(ws=None), dict(ws=OFF), dict(nbytes=WS - 1)):
