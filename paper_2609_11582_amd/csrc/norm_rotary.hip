@@ -5,16 +5,16 @@
 //   dx = r (w g - x r^2 mean(w g x)),   dw = sum over rows of g x r.
 // All in fp32, each row rounded once; the row's sums go through the 8 lanes that carry it.
 //
-// Bound: memory (one read and one write of every row; two reads and one write backwards): 32768 tokens x 32 heads 105 us, 5.1
-// TB/s (a large copy 5.17); backwards 8192 tokens x 32 heads 35 us, 4 sequences of up to 2999 tokens x 18 heads 25 us, and
-// 4 us for the weights' sum. One token is bound by its launch (3.5 us, 12 a call). The split is the rotation's: a
+// Bound: memory (one read and one write of every row; two reads and one write backwards): 32768 tokens x 32 heads 100 us, 5.3
+// TB/s (a large copy 5.17); backwards, with the weights' sum, 8192 tokens x 32 heads 47 us, 4 sequences of up to 2999 tokens x 18
+// heads 35 us, of which the sum and its launch are 7 to 9. One token is bound by its launch (3.5 us, 12 a call). The split is the rotation's: a
 // work-group takes T tokens, whose sines and cosines go to LDS once; a lane keeps those of its 8 pairs, times the
 // weights, in registers for all heads of a kind; eight lanes carry a row, 32 bytes each way.
 //
 // The weights' gradient: a lane adds up its 16 channels over all the rows that it meets, a work-group its lanes, and
 // a second launch the work-groups, all in a fixed order: the same inputs give the same bits. So the backward's
-// work-groups are few (kNormParts: one round of the GPU; 8192 tokens x 32 heads 38.5 us, with 1024 40.4, 512 37.6, but 4 sequences of
-// 2999 x 18 heads 29.7, 29.7 and 30.3) and take one tile after the other.
+// work-groups are few (kNormParts: one round of the GPU; 8192 tokens x 32 heads, inputs in the last-level cache, 38.5 us, with 1024
+// 40.4, 512 37.6, but 4 sequences of 2999 x 18 heads 29.7, 29.7 and 30.3) and take one tile after the other.
 #include <algorithm>
 
 #include "q8.hpp"
@@ -25,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kRows = 4, kGradRows = 2;  // rows that a lane loads at once
 
 // Cosine and sine of the pairs of tokens t0 .. t0 + nt - 1 of sequence b
 template <int T>
@@ -119,10 +118,11 @@ template <bool kBf16, bool kAdjacent, int T>
 __global__ __launch_bounds__(kThreads) void k_norm_rotary(NormRotaryArgs a, int ntile) {
   __shared__ __attribute__((aligned(16))) float2 cs[T][64];
   constexpr int kHeads = 8 / T, kStep = kWaves * kHeads;  // heads of a wave at once, of the work-group
+  constexpr int kRows = T == 8 ? 2 : 4;                   // rows that a lane loads at once
   const RotaryArgs& p = a.r;
   const int tid = threadIdx.x, lane = tid & 63, heads = p.hq + p.hk;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j = lane & 7, t = T == 1 ? 0 : lane >> 3, h0 = T == 1 ? wave * kHeads + (lane >> 3) : wave;
+  const int j = lane & 7, t = (lane >> 3) % T, h0 = wave * kHeads + (lane >> 3) / T;
   for (int64_t unit = blockIdx.x; unit < (int64_t)ntile * p.nb; unit += gridDim.x) {
     const int bi = (int)(unit / ntile), t0 = (int)(unit % ntile) * T, b = p.b0 + bi;
     const int nt = min(p.lens.lens[bi] - t0, T);
@@ -175,11 +175,11 @@ template <bool kBf16, bool kAdjacent, int T>
 __global__ __launch_bounds__(kThreads) void k_norm_rotary_grad(NormRotaryArgs a, int ntile, int part0) {
   __shared__ __attribute__((aligned(16))) float2 cs[T][64];
   __shared__ float sums[kWaves][2 * kD];
-  constexpr int kHeads = 8 / T, kStep = kWaves * kHeads;
+  constexpr int kHeads = 8 / T, kStep = kWaves * kHeads, kGradRows = T == 4 ? 1 : 2;
   const RotaryArgs& p = a.r;
   const int tid = threadIdx.x, lane = tid & 63, heads = p.hq + p.hk;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j = lane & 7, t = T == 1 ? 0 : lane >> 3, h0 = T == 1 ? wave * kHeads + (lane >> 3) : wave;
+  const int j = lane & 7, t = (lane >> 3) % T, h0 = wave * kHeads + (lane >> 3) / T;
   float dw[2][16] = {};
   for (int64_t unit = blockIdx.x; unit < (int64_t)ntile * p.nb; unit += gridDim.x) {
     const int bi = (int)(unit / ntile), t0 = (int)(unit % ntile) * T, b = p.b0 + bi;
@@ -271,20 +271,39 @@ __global__ __launch_bounds__(kSumCols* kSumRows) void k_norm_weight_sum(const fl
   if (to) to[at & (kD - 1)] = (float)v;
 }
 
-// One token to a work-group up to some five work-groups for each compute unit, as in the rotation
-constexpr int kFewTokens = 1280;
-int tokens_of(int max_len, int nb) { return (int64_t)max_len * nb <= kFewTokens ? 1 : 8; }
+// Tokens of a work-group (32, 18 and 5 heads in all, token by token in memory, us of a call in a graph).
+// * 1 where there are few tokens, and heads enough for its lanes: 128 tokens 3.4 2.8 3.4, with 4 4.0 3.7 2.8; 512 4.3 3.3 3.7 and 4.4
+//   3.9 2.9; 640 4.9 3.7 3.8 and 4.8 3.9 3.0; 1280 9.4 5.9 6.2 and 7.6 5.0 3.3.
+// * 4 beyond, 8 where tokens are many and the query heads no more than one load of 4 rows for each of 4 waves: 1280 tokens 8.2 5.3
+//   3.8 with 8, 2560 10.0 7.7 3.8 with 4 and 11.2 8.4 4.2 with 8; 8192 30.4 16.5 10.3 and 30.4 14.6 7.6; 32768 95 67 29 and 103 60 20.
+int tokens_of(const NormRotaryArgs& a, int max_len) {
+  const int64_t tokens = (int64_t)max_len * a.r.nb;
+  if (tokens <= 512 && a.r.hq + a.r.hk > 8) return 1;
+  return tokens <= 2560 || a.r.hq > 16 ? 4 : 8;
+}
+// Backwards the work-groups are one round, so that some take a tile more than others: 4 where that leaves the longest of them fewer
+// tokens than 8. Us: 128 tokens 8.0 7.1 7.9 with 1, 8.6 7.9 6.7 with 4; 320 9.8 8.8 9.2 and 9.2 8.4 7.1; 1024 17.8 14.6 14.8 and 12.8
+// 11.1 8.0, with 8 14.4 11.6 8.1; 2560 19.4 14.9 10.3 with 4 and 20.3 16.1 10.6 with 8, 4096 26.3 18.0 13.0 and 24.8 16.8 11.3 (two tiles
+// against one), 8192 46.7 30.8 15.9 and 48.0 31.0 15.9.
+int grad_tokens_of(const NormRotaryArgs& a, int max_len) {
+  const int64_t tokens = (int64_t)max_len * a.r.nb;
+  if (tokens <= 256 && a.r.hq + a.r.hk > 8) return 1;
+  auto most = [&](int T) { return ((int64_t)((max_len + T - 1) / T) * a.r.nb + kNormParts - 1) / kNormParts * T; };
+  return most(4) < most(8) ? 4 : 8;
+}
 
 template <bool kBf16, bool kAdjacent>
 hipError_t launch(const NormRotaryArgs& a, int max_len, int part0, int groups, hipStream_t s) {
-  const int T = tokens_of(max_len, a.r.nb), ntile = (max_len + T - 1) / T;
+  const int T = groups ? grad_tokens_of(a, max_len) : tokens_of(a, max_len), ntile = (max_len + T - 1) / T;
   const dim3 block(kThreads);
   if (groups) {
     if (T == 1) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 1>), dim3(groups), block, 0, s, a, ntile, part0);
+    else if (T == 4) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 4>), dim3(groups), block, 0, s, a, ntile, part0);
     else hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 8>), dim3(groups), block, 0, s, a, ntile, part0);
   } else {
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)ntile * a.r.nb, 1 << 20));
     if (T == 1) hipLaunchKernelGGL((k_norm_rotary<kBf16, kAdjacent, 1>), grid, block, 0, s, a, ntile);
+    else if (T == 4) hipLaunchKernelGGL((k_norm_rotary<kBf16, kAdjacent, 4>), grid, block, 0, s, a, ntile);
     else hipLaunchKernelGGL((k_norm_rotary<kBf16, kAdjacent, 8>), grid, block, 0, s, a, ntile);
   }
   return hipGetLastError();
@@ -302,10 +321,10 @@ hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, h
   return max_len == 0 ? hipSuccess : dispatch(a, dtype, max_len, 0, 0, s);
 }
 
-int norm_rotary_parts(int max_len, int nb, int launches) {
+int norm_rotary_parts(const NormRotaryArgs& a, int max_len, int launches) {
   if (max_len == 0) return 0;
-  const int T = tokens_of(max_len, nb);
-  return (int)std::min<int64_t>((int64_t)((max_len + T - 1) / T) * nb, std::max(kNormParts / launches, 1));
+  const int T = grad_tokens_of(a, max_len);
+  return (int)std::min<int64_t>((int64_t)((max_len + T - 1) / T) * a.r.nb, std::max(kNormParts / launches, 1));
 }
 
 hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s) {

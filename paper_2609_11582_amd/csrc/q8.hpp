@@ -33,7 +33,7 @@ struct NormRotaryArgs {
 };
 constexpr int kNormParts = 768;   // work-groups of a backward pass at most: three to a compute unit, what their registers allow
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, hipStream_t s);
-int norm_rotary_parts(int max_len, int nb, int launches);  // work-groups of one of the launches of a backward pass
+int norm_rotary_parts(const NormRotaryArgs& a, int max_len, int launches);  // work-groups of one of the launches of a backward pass
 hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s);
 hipError_t launch_norm_weight_sum(const float* parts, int n, float* dq_weight, float* dk_weight, hipStream_t s);
 

@@ -320,7 +320,7 @@ okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t 
   const int launches = (batch + kMaxLenArgs - 1) / kMaxLenArgs;
   int parts = 0;
   st = rotary_launches(a.r, batch, lens_host, [&](int most) {
-    const int groups = norm_rotary_parts(most, a.r.nb, launches), part0 = parts;
+    const int groups = norm_rotary_parts(a, most, launches), part0 = parts;
     parts += groups;
     return launch_norm_rotary_grad(a, dtype, most, part0, groups, static_cast<hipStream_t>(stream));
   });

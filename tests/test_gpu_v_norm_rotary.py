@@ -67,7 +67,8 @@ def _backward(par, q, k, pos, dqk, lens=None, flags=0, ws=None, stream=None):
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("adjacent", [False, True])
-@pytest.mark.parametrize("B, hq, hk, n", [(1, 28, 4, 1), (3, 7, 1, 37), (1, 1, 1, 8), (2, 16, 2, 9), (1, 33, 5, 2), (2, 6, 3, 700)])
+@pytest.mark.parametrize("B, hq, hk, n", [(1, 28, 4, 1), (3, 7, 1, 37), (1, 1, 1, 8), (2, 16, 2, 9), (1, 33, 5, 2), (2, 6, 3, 700),
+                                         (1, 12, 2, 301), (1, 3, 2, 4101), (1, 17, 2, 2571)])
 def test_forward_and_gradient(dtype, adjacent, B, hq, hk, n):
     import torch
 
