@@ -183,8 +183,11 @@ inline bool q8_wide_is_faster(int64_t rows, int64_t units16, int64_t units64, in
 // * One split up to 4 rounds of a block for each wave, which saves the merge launch (on the device; the host has one launch
 //   less to make too): 300 tokens 8.4 -> 6.2 us, 512 8.5 -> 7.0, 1024 8.6 -> 9.2. Windows, whose walk waits for the length: up to 7 (4 heads,
 //   windows of 1024: 1 slot 12.3 -> 9.6 us, 16 slots 12.8 -> 9.8, 64 slots 20.5 -> 14.1; of 1500 12.0 -> 11.3; of 1900, 8 rounds, 12.0 ->
-//   13.1). Trees, which
-//   are merged in any case, up to 3: 300 tokens 13.6 -> 11.8, 1000 (4 rounds) 13.7 -> 14.0.
+//   13.1), and more where many even tiles share the GPU's bandwidth anyway: as many times 7 as there are 64 tiles, and without a limit
+//   from 160 tiles on (4 heads, windows of 2000: 24 slots 17.6 -> 16.6, 32 20.8 -> 16.8, 48 25.4 -> 19.3, 64 29.5 -> 24.8; of 4096:
+//   32 28.1 and 27.8, 48 40.5 -> 32.8; of 8192: 32 47 and 55, 40 63 -> 62, 48 87 -> 72; 48 sequences of 3000 to 6000 46 -> 40).
+//   Trees, which are merged in any case, up to 3: 300 tokens 13.6 -> 11.8, 1000 (4 rounds) 13.7 -> 14.0; and all from 160 tiles on that
+//   are even (4 heads x 8192 tokens: 40 slots 66.8 and 67.6, 48 87.8 -> 77.2, 64 103 -> 100; not 96 of 1000 to 2000, 31 and 36).
 // * At most 64 splits, as more cost the merge what they save (32768 tokens, 4 heads: 11.2 us, with 128 splits 13.1),
 //   but 128 where 64 would leave compute units idle for more than 4 rounds (131072 tokens, 1 head: 18.3 -> 14.4 us).
 // * Tiles of 128 columns where short sequences leave compute units idle: a tile of half the columns takes half the time
@@ -269,7 +272,9 @@ inline void q8_plan(Q8Plan& p, int B, int H, int G, int most_new, const int32_t*
     if (fits(mid)) hi = mid;
     else lo = mid + 1;
   }
-  const int64_t alone = span == 1 ? 7 : span == 2 ? 3 : 4;
+  int64_t alone = span == 1 ? 7 : span == 2 ? 3 : 4;
+  if (span && few && units16 <= kQ8Groups && longest * units16 * 4 <= work16 * (span == 1 ? 6 : 5))
+    alone = units16 >= 160 ? (longest + round - 1) / round : span == 1 ? std::max(alone, alone * units16 / 64) : alone;
   if (few && longest <= alone * round) hi = alone;
   const bool idle = units * 64 < 256 && longest > 64 * 4 * round;
   const int64_t cap = idle ? kQ8MaxSplits : 64;

@@ -500,6 +500,18 @@ def test_windows_past_any_sequence():
     _check_tree(c, a, lens, qd, k, v, visible, [9] * 3, "int8", "fp16", "largest window of a tree")
 
 
+def test_many_even_slots_take_one_split():
+    """160 tiles of more rounds than a split has elsewhere, and one slot that is longer than the others."""
+    for lens in ([2100] * 160, [2100] * 159 + [4000]):
+        c = _filled(160, 1, 2, lens, 64, "int8", "fp16", 171)
+        q = _rows(172, 160, 2, 1, 128)
+        _check_window(c, _window(c, lens, q, [1] * 160, 2500, 3), lens, q, [1] * 160, 2500, 3, "int8", "fp16", f"even slots {lens[-1]}")
+        n_draft = [2] * 159 + [1]
+        qd, k, v = _drafts(173, 160, 1, 2, 2, "fp16")
+        visible = _masks([[-1, 0][:m] for m in n_draft], 2)
+        _check_tree(c, _tree(c, lens, qd, k, v, visible, n_draft), lens, qd, k, v, visible, n_draft, "int8", "fp16", f"even trees {lens[-1]}")
+
+
 # ---- as they are used ----------------------------------------------------------------------------
 
 
