@@ -8,8 +8,9 @@
 // there, straight into the matrix instructions (32x32x16, two tiles of 32 columns); no barrier in the loop.
 //  * The columns' sums are 128 registers. The query operands do not fit beside them: they lie in LDS (16 KB) and are read for
 //    every block, 1 KB for each matrix instruction of the scores.
-//  * int8 keys enter as fp16 subnormals, (code + 128) 2^-24, one permutation of bytes: sum q code = 2^24 dot - 128 sum q, whose
-//    second term joins `off`.
+//  * Keys enter as their codes, widened exactly: an offset on int8's, taken off again behind the product, would put a score's error at
+//    2^-24 of 128 scale |sum q| in place of scale sum |q code|, 10 times the error that the other kernels' roundings allow at
+//    queries of mean 20 against blocks with one channel of 1000.
 //  * The work-groups are numbered through, those of a slot, head and split side by side on one XCD, so that its L2 serves the
 //    tiles that read the same codes, and no XCD has more of them than others (a ragged batch launched as slots x splits
 //    put 33 on some XCDs' 32 compute units, which took a second round: 62 us for 8 slots of 133 to 175 columns).
@@ -28,19 +29,6 @@ constexpr int kTiles = kQ8WideCols / 32;
 constexpr int kHalfRow = kD / 2 + 4;           // floats of a combine row: 8 rows fall into all banks
 constexpr float kLeastWeight = -60.0f;         // log2 of the weight at the reference m, as in the prompt kernel
 
-// eight key codes as a matrix operand: e4m3 as they are, int8 as (code + 128) 2^-24
-template <int kFmt>
-__device__ __forceinline__ half8 key8(uint32_t a, uint32_t b) {
-  if constexpr (kFmt == OKVQ_Q8_E4M3) {
-    return widen8<kFmt>(a, b);
-  } else {
-    a ^= 0x80808080u;
-    b ^= 0x80808080u;
-    return __builtin_bit_cast(half8, make_uint4(__builtin_amdgcn_perm(0u, a, 0x0c010c00u), __builtin_amdgcn_perm(0u, a, 0x0c030c02u),
-                                                __builtin_amdgcn_perm(0u, b, 0x0c010c00u), __builtin_amdgcn_perm(0u, b, 0x0c030c02u)));
-  }
-}
-
 struct WideShared {
   union {
     uint4 qop[8][kTiles][64];                                    // contraction step, columns, lane
@@ -48,7 +36,7 @@ struct WideShared {
   };
   float wM[kWaves][kQ8WideCols], wm[kWaves][kQ8WideCols], wl[kWaves][kQ8WideCols];
   floatx4 total[kQ8WideCols];                                    // (M, m, l, 0) of all waves
-  float qscale[kQ8WideCols], corr[kQ8WideCols];
+  float qscale[kQ8WideCols];
   int vis[kQ8WideCols], from[kQ8WideCols];                       // what a column's row sees
 };
 
@@ -144,12 +132,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
       x = fmaxf(x, fdpp<0x4E>(x));
       return fmaxf(x, fswap4(x));
     });
-    float sum = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += (float)op[0][e] + (float)op[1][e];
-    sum += fdpp<0xB1>(sum);
-    sum += fdpp<0x4E>(sum);
-    sum += fswap4(sum);
     // step 2 (part / 2) + e, lanes of half part % 2
 #pragma unroll
     for (int e = 0; e < 2; ++e) sh.qop[2 * (part >> 1) + e][qcol >> 5][32 * (part & 1) + (qcol & 31)] = __builtin_bit_cast(uint4, op[e]);
@@ -158,19 +140,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
       sh.vis[qcol] = sight.end;
       sh.from[qcol] = sight.from;
       sh.qscale[qcol] = fabsf(p.qscale) * f;
-      sh.corr[qcol] = 128.0f * sum;
     }
   }
   __syncthreads();
 
-  float m[kTiles], M[kTiles], l[kTiles], qs[kTiles], corr[kTiles];
+  float m[kTiles], M[kTiles], l[kTiles], qs[kTiles];
   floatx16 acc[kTiles][4];  // channel 32 j + 8 (e / 4) + 4 half + e % 4 of the column
 #pragma unroll
   for (int ct = 0; ct < kTiles; ++ct) {
     m[ct] = M[ct] = kNoScore;
     l[ct] = 0.0f;
     qs[ct] = sh.qscale[32 * ct + col];
-    corr[ct] = sh.corr[32 * ct + col];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -194,7 +174,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
       const uint4 w = k[kk >> 1];
-      const half8 key = kk & 1 ? key8<kFmt>(w.z, w.w) : key8<kFmt>(w.x, w.y);
+      const half8 key = kk & 1 ? widen8<kFmt>(w.z, w.w) : widen8<kFmt>(w.x, w.y);
 #pragma unroll
       for (int ct = 0; ct < kTiles; ++ct)
         s[ct] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, __builtin_bit_cast(half8, sh.qop[kk][ct][lane]), s[ct], 0, 0, 0);
@@ -229,7 +209,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
       for (int j = 0; j < 4; ++j) any |= v[j][0].x | v[j][0].y | v[j][1].x | v[j][1].y;
       dead = !__any((any & 0x7f7f7f7fu) != 0);
     }
-    float sc[kTiles], shift[kTiles], high[kTiles], reach[kTiles];
+    float sc[kTiles], high[kTiles], reach[kTiles];
     bool moves = false;
 #pragma unroll
     for (int ct = 0; ct < kTiles; ++ct) {
@@ -237,12 +217,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
 #pragma unroll
       for (int e = 1; e < 16; ++e) x = fmaxf(x, s[ct][e]);
       sc[ct] = fmaxf(scale * qs[ct], 1e-37f);  // above zero: a masked dot stays -inf
-      shift[ct] = 0.0f;
-      if constexpr (kFmt == OKVQ_Q8_INT8) {
-        shift[ct] = corr[ct] * sc[ct];
-        sc[ct] *= 0x1p24f;
-      }
-      high[ct] = __builtin_fmaf(max32(x), sc[ct], -shift[ct]);
+      high[ct] = max32(x) * sc[ct];
       reach[ct] = dead ? -__builtin_inff() : high[ct] + lv;
       moves |= high[ct] > m[ct] + kLazy || reach[ct] > M[ct] + kLazy;
     }
@@ -264,12 +239,12 @@ __global__ __launch_bounds__(kThreads, 2) void k_q8_wide(Q8AttendArgs p, Q8Units
     for (int ct = 0; ct < kTiles; ++ct) {
       // zero codes take any finite weight. Values too small beside others for a weight in fp16 take one that is zero there and
       // still adds to the sum in fp32
-      const float off = dead ? -m[ct] : fmaxf(lv + kWeightExp - M[ct], kLeastWeight - m[ct]), at = off - shift[ct];
+      const float off = dead ? -m[ct] : fmaxf(lv + kWeightExp - M[ct], kLeastWeight - m[ct]);
       float sum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ct][e], sc[ct], at));
-        const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ct][e + 1], sc[ct], at));
+        const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ct][e], sc[ct], off));
+        const float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ct][e + 1], sc[ct], off));
         sum += w0 + w1;
         w[ct][e >> 1] = pack_f16(w0, w1);
       }
