@@ -12,9 +12,10 @@
 // weights, in registers for all heads of a kind; eight lanes carry a row, 32 bytes each way.
 //
 // The weights' gradient: a lane adds up its 16 channels over all the rows that it meets, a work-group its lanes, and
-// a second launch the work-groups, all in a fixed order: the same inputs give the same bits. So the backward's
+// a last launch the work-groups, all in a fixed order: the same inputs give the same bits. So the backward's
 // work-groups are few (kNormParts: one round of the GPU; 8192 tokens x 32 heads, inputs in the last-level cache, 38.5 us, with 1024
-// 40.4, 512 37.6, but 4 sequences of 2999 x 18 heads 29.7, 29.7 and 30.3) and take one tile after the other.
+// 40.4, 512 37.6, but 4 sequences of 2999 x 18 heads 29.7, 29.7 and 30.3) and take one tile after the other. Batches of more than
+// 256 sequences take a launch for each 256, which all use the same work-groups' sums: later ones add to what is there.
 #include <algorithm>
 
 #include "q8.hpp"
@@ -170,9 +171,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotary(NormRotaryArgs a, int 
   }
 }
 
-// Rows of gradients, and the work-group's part of the weights' [q, k][128] at a.parts + 256 (part0 + work-group)
+// Rows of gradients, and the work-group's part of the weights' [q, k][128] at a.parts + 256 work-group: added to what an earlier
+// launch left there in the first `kept` of them, stored in the others
 template <bool kBf16, bool kAdjacent, int T>
-__global__ __launch_bounds__(kThreads) void k_norm_rotary_grad(NormRotaryArgs a, int ntile, int part0) {
+__global__ __launch_bounds__(kThreads) void k_norm_rotary_grad(NormRotaryArgs a, int ntile, int kept) {
   __shared__ __attribute__((aligned(16))) float2 cs[T][64];
   __shared__ float sums[kWaves][2 * kD];
   constexpr int kHeads = 8 / T, kStep = kWaves * kHeads, kGradRows = T == 4 ? 1 : 2;
@@ -250,7 +252,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_rotary_grad(NormRotaryArgs a,
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) v += sums[w][tid];
   static_assert(kThreads == 2 * kD, "a thread for each weight");
-  a.parts[(int64_t)(part0 + blockIdx.x) * (2 * kD) + tid] = v;
+  float* at = a.parts + (int64_t)blockIdx.x * (2 * kD) + tid;
+  *at = (int)blockIdx.x < kept ? *at + v : v;
 }
 
 // The parts' sum: a work-group takes 16 weights, 64 threads each, which hold 64 bits
@@ -293,13 +296,13 @@ int grad_tokens_of(const NormRotaryArgs& a, int max_len) {
 }
 
 template <bool kBf16, bool kAdjacent>
-hipError_t launch(const NormRotaryArgs& a, int max_len, int part0, int groups, hipStream_t s) {
+hipError_t launch(const NormRotaryArgs& a, int max_len, int kept, int groups, hipStream_t s) {
   const int T = groups ? grad_tokens_of(a, max_len) : tokens_of(a, max_len), ntile = (max_len + T - 1) / T;
   const dim3 block(kThreads);
   if (groups) {
-    if (T == 1) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 1>), dim3(groups), block, 0, s, a, ntile, part0);
-    else if (T == 4) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 4>), dim3(groups), block, 0, s, a, ntile, part0);
-    else hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 8>), dim3(groups), block, 0, s, a, ntile, part0);
+    if (T == 1) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 1>), dim3(groups), block, 0, s, a, ntile, kept);
+    else if (T == 4) hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 4>), dim3(groups), block, 0, s, a, ntile, kept);
+    else hipLaunchKernelGGL((k_norm_rotary_grad<kBf16, kAdjacent, 8>), dim3(groups), block, 0, s, a, ntile, kept);
   } else {
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)ntile * a.r.nb, 1 << 20));
     if (T == 1) hipLaunchKernelGGL((k_norm_rotary<kBf16, kAdjacent, 1>), grid, block, 0, s, a, ntile);
@@ -309,10 +312,10 @@ hipError_t launch(const NormRotaryArgs& a, int max_len, int part0, int groups, h
   return hipGetLastError();
 }
 
-hipError_t dispatch(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s) {
+hipError_t dispatch(const NormRotaryArgs& a, int dtype, int max_len, int kept, int groups, hipStream_t s) {
   const bool adj = (a.r.flags & OKVQ_ROTARY_ADJACENT) != 0;
-  if (dtype == OKVQ_BF16) return adj ? launch<true, true>(a, max_len, part0, groups, s) : launch<true, false>(a, max_len, part0, groups, s);
-  return adj ? launch<false, true>(a, max_len, part0, groups, s) : launch<false, false>(a, max_len, part0, groups, s);
+  if (dtype == OKVQ_BF16) return adj ? launch<true, true>(a, max_len, kept, groups, s) : launch<true, false>(a, max_len, kept, groups, s);
+  return adj ? launch<false, true>(a, max_len, kept, groups, s) : launch<false, false>(a, max_len, kept, groups, s);
 }
 
 }  // namespace
@@ -321,14 +324,14 @@ hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, h
   return max_len == 0 ? hipSuccess : dispatch(a, dtype, max_len, 0, 0, s);
 }
 
-int norm_rotary_parts(const NormRotaryArgs& a, int max_len, int launches) {
+int norm_rotary_parts(const NormRotaryArgs& a, int max_len) {
   if (max_len == 0) return 0;
   const int T = grad_tokens_of(a, max_len);
-  return (int)std::min<int64_t>((int64_t)((max_len + T - 1) / T) * a.r.nb, std::max(kNormParts / launches, 1));
+  return (int)std::min<int64_t>((int64_t)((max_len + T - 1) / T) * a.r.nb, kNormParts);
 }
 
-hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s) {
-  return groups == 0 ? hipSuccess : dispatch(a, dtype, max_len, part0, groups, s);
+hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int kept, int groups, hipStream_t s) {
+  return groups == 0 ? hipSuccess : dispatch(a, dtype, max_len, kept, groups, s);
 }
 
 hipError_t launch_norm_weight_sum(const float* parts, int n, float* dq_weight, float* dk_weight, hipStream_t s) {

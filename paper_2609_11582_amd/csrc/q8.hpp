@@ -29,12 +29,13 @@ struct NormRotaryArgs {
   const float* k_weight;
   float eps;
   okvq_rows q_grad, k_grad; // backward: gradients of what the forward pass wrote
-  float* parts;             // backward: [n][2][128] sums of work-groups
+  float* parts;             // backward: [kNormParts][2][128] sums of work-groups
 };
 constexpr int kNormParts = 768;   // work-groups of a backward pass at most: three to a compute unit, what their registers allow
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, hipStream_t s);
-int norm_rotary_parts(const NormRotaryArgs& a, int max_len, int launches);  // work-groups of one of the launches of a backward pass
-hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int part0, int groups, hipStream_t s);
+int norm_rotary_parts(const NormRotaryArgs& a, int max_len);  // work-groups of one of the launches of a backward pass
+// kept: work-groups whose sums hold those of earlier launches
+hipError_t launch_norm_rotary_grad(const NormRotaryArgs& a, int dtype, int max_len, int kept, int groups, hipStream_t s);
 hipError_t launch_norm_weight_sum(const float* parts, int n, float* dq_weight, float* dk_weight, hipStream_t s);
 
 // ---- 8-bit cache ---------------------------------------------------------------------------------

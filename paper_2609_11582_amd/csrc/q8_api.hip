@@ -317,12 +317,11 @@ okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t 
   a.q_grad = q ? *q_grad : okvq_rows{};
   a.k_grad = k ? *k_grad : okvq_rows{};
   a.parts = static_cast<float*>(workspace);
-  const int launches = (batch + kMaxLenArgs - 1) / kMaxLenArgs;
   int parts = 0;
   st = rotary_launches(a.r, batch, lens_host, [&](int most) {
-    const int groups = norm_rotary_parts(a, most, launches), part0 = parts;
-    parts += groups;
-    return launch_norm_rotary_grad(a, dtype, most, part0, groups, static_cast<hipStream_t>(stream));
+    const int groups = norm_rotary_parts(a, most), kept = parts;
+    parts = std::max(parts, groups);
+    return launch_norm_rotary_grad(a, dtype, most, kept, groups, static_cast<hipStream_t>(stream));
   });
   if (st != OKVQ_OK) return st;
   return hip_status(launch_norm_weight_sum(a.parts, parts, q ? dq_weight : nullptr, k ? dk_weight : nullptr,
