@@ -1,0 +1,46 @@
+"""Windows and trees over the 8-bit cache at shapes that take each kernel in each role (test_q8_span_shapes.py holds the plan to that):
+the prompt kernel's splits, whose records a merge joins. Tolerances as in test_gpu_w_q8_window_tree.py."""
+
+import numpy as np
+import pytest
+import q8_span_shapes as sh
+
+from test_gpu_u_q8_cache import _filled, _rows
+from test_gpu_w_q8_window_tree import _check_tree, _check_window, _drafts, _masks, _parents, _tree, _window
+
+pytestmark = pytest.mark.gpu
+
+
+def _ids(shapes):
+    return [s.name.replace(" ", "-") for s in shapes]
+
+
+def _tree_inputs(s, dtype, seed):
+    n = max(s.n)
+    q, k, v = _drafts(seed, len(s.lens), s.H, s.Hq, n, dtype)
+    visible = _masks([_parents(np.random.default_rng(seed + b), m, "any") for b, m in enumerate(s.n)], n)
+    for b, m in enumerate(s.n):
+        q[b, :, m:] = k[b, :, m:] = v[b, :, m:] = float("nan")
+    return q, k, v, visible
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("s", sh.SPLIT_TREES, ids=_ids(sh.SPLIT_TREES))
+def test_split_trees_of_the_prompt_kernel(fmt, dtype, s):
+    c = _filled(len(s.lens), s.H, s.Hq, s.lens, 64, fmt, dtype, 191)
+    q, k, v, visible = _tree_inputs(s, dtype, 192)
+    out = _tree(c, s.lens, q, k, v, visible, s.n, s.window, s.sinks)
+    _check_tree(c, out, s.lens, q, k, v, visible, s.n, fmt, dtype, f"split tree {fmt} {dtype} {s.name}", s.window, s.sinks,
+                rows=np.array([0, 1, 18, 19, 36, 37, 63, 100, 128, 199, 255]))
+
+
+@pytest.mark.parametrize("fmt, dtype", [("int8", "fp16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("s", sh.SPLIT_WINDOWS, ids=_ids(sh.SPLIT_WINDOWS))
+def test_split_windows_of_the_prompt_kernel(fmt, dtype, s):
+    c = _filled(len(s.lens), s.H, s.Hq, s.lens, 64, fmt, dtype, 193)
+    q = _rows(194, len(s.lens), s.Hq, max(s.n) + 1, 128, dtype=dtype, scale=1.5)  # a row more than any sequence has
+    for b, m in enumerate(s.n):
+        q[b, :, m:] = float("nan")
+    out = _window(c, s.lens, q, s.n, s.window, s.sinks)
+    _check_window(c, out, s.lens, q, s.n, s.window, s.sinks, fmt, dtype, f"split window {fmt} {dtype} {s.name}",
+                  rows=np.array([0, 1, 18, 19, 31, 32, 100, 199, 255, 256, 499, 511]))
