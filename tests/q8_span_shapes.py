@@ -18,3 +18,18 @@ SPLIT_WINDOWS = [
     Shape("4 chunks of 512", 2, 16, [6000, 5900, 6003, 5800], [512, 500, 512, 511], 4096, 64, 256, 2),
     Shape("one long chunk of 3", 4, 28, [1500, 300, 333], [200, 190, 200], 1200, 5, 128, 3),
 ]
+# pages that no row sees, in each kernel
+HIDDEN_WINDOWS = [
+    Shape("split", 1, 7, [2000], [1], 300, 10, 16, 1),
+    Shape("wide", 1, 16, [20000], [20], 15000, 10, 64, 30),
+    Shape("prompt, halves", 4, 28, [3000], [2500], 300, 10, 128, 1),
+    Shape("prompt, halves of a longer sequence", 4, 28, [6000], [2500], 300, 10, 128, 1),
+    Shape("prompt", 4, 28, [3000], [1200], 300, 10, 256, 1),
+    Shape("prompt, splits", 2, 16, [6000] * 4, [512] * 4, 4096, 40, 256, 2),
+]
+HIDDEN_TREES = [
+    Shape("split", 1, 7, [2000], [2], 300, 10, 16, 1),
+    Shape("wide", 1, 16, [30000], [16], 17000, 10, 64, 34),
+    Shape("prompt, halves, splits", 4, 28, [2500, 300, 333], [200, 190, 200], 1200, 5, 128, 3),
+    Shape("prompt, splits", 4, 32, [7000] * 4, [256] * 4, 4500, 70, 256, 2),
+]

@@ -1,12 +1,13 @@
 """Windows and trees over the 8-bit cache at shapes that take each kernel in each role (test_q8_span_shapes.py holds the plan to that):
-the prompt kernel's splits, whose records a merge joins. Tolerances as in test_gpu_w_q8_window_tree.py."""
+the prompt kernel's splits, whose records a merge joins, and, for every kernel, pages that no row sees. Tolerances as in
+test_gpu_w_q8_window_tree.py."""
 
 import numpy as np
 import pytest
 import q8_span_shapes as sh
 
 from test_gpu_u_q8_cache import _filled, _rows
-from test_gpu_w_q8_window_tree import _check_tree, _check_window, _drafts, _masks, _parents, _tree, _window
+from test_gpu_w_q8_window_tree import _check_tree, _check_window, _drafts, _masks, _np, _parents, _tree, _window
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,37 @@ def test_split_windows_of_the_prompt_kernel(fmt, dtype, s):
     out = _window(c, s.lens, q, s.n, s.window, s.sinks)
     _check_window(c, out, s.lens, q, s.n, s.window, s.sinks, fmt, dtype, f"split window {fmt} {dtype} {s.name}",
                   rows=np.array([0, 1, 18, 19, 31, 32, 100, 199, 255, 256, 499, 511]))
+
+
+def _hide(c, s, first_seen):
+    """Fill the pages behind the sinks and before the first that some row of the slot sees with NaN scales and codes of 0x7f."""
+    hidden = 0
+    for b, at in enumerate(first_seen):
+        for page in c["block_table"][b, -(-s.sinks // 64):max(at, 0) // 64].tolist():
+            hidden += 1
+            for f in ("k_scale", "v_scale"):
+                c[f][0, page] = float("nan")
+            for f in ("k_codes", "v_codes"):
+                c[f][0, page] = 0x7f
+    assert hidden >= 2
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("s", sh.HIDDEN_WINDOWS, ids=_ids(sh.HIDDEN_WINDOWS))
+def test_windows_do_not_read_hidden_pages(fmt, s):
+    c = _filled(len(s.lens), s.H, s.Hq, s.lens, 64, fmt, "fp16", 195)
+    q = _rows(196, len(s.lens), s.Hq, max(s.n), 128)
+    want = _np(_window(c, s.lens, q, s.n, s.window, s.sinks))
+    _hide(c, s, [L - m + 1 - s.window for L, m in zip(s.lens, s.n)])
+    assert np.isfinite(want).all() and np.array_equal(_np(_window(c, s.lens, q, s.n, s.window, s.sinks)), want)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("s", sh.HIDDEN_TREES, ids=_ids(sh.HIDDEN_TREES))
+def test_trees_do_not_read_hidden_pages(fmt, s):
+    c = _filled(len(s.lens), s.H, s.Hq, s.lens, 64, fmt, "fp16", 197)
+    q, k, v, visible = _tree_inputs(s, "fp16", 198)
+    want = _np(_tree(c, s.lens, q, k, v, visible, s.n, s.window, s.sinks))
+    _hide(c, s, [L + 1 - s.window for L in s.lens])  # of a row that names one draft
+    again = _np(_tree(c, s.lens, q, k, v, visible, s.n, s.window, s.sinks))
+    assert np.isfinite(want).all() and np.array_equal(again, want)

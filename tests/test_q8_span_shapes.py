@@ -22,6 +22,6 @@ def planned(tmp_path_factory):
     return plan
 
 
-@pytest.mark.parametrize("span, shapes", [(1, sh.SPLIT_WINDOWS), (2, sh.SPLIT_TREES)])
+@pytest.mark.parametrize("span, shapes", [(1, sh.SPLIT_WINDOWS), (1, sh.HIDDEN_WINDOWS), (2, sh.SPLIT_TREES), (2, sh.HIDDEN_TREES)])
 def test_shapes_take_their_kernel(planned, span, shapes):
     assert planned(span, shapes) == [(s.cols, s.most) for s in shapes]
