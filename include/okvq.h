@@ -519,7 +519,8 @@ size_t okvq_norm_rotary_workspace_bytes(int32_t batch, int32_t n_tokens);
  *   dq, dk     device rows, as the outputs of okvq_rotary; one may be its own gradient or input with the same strides (in
  *              place) and may not overlap a row that is read otherwise. Rows t >= lens_host[b] are left as they were
  *   dq_weight, dk_weight  device fp32 [128], one each, overwritten with the sums over all rows (zero where there are none), in an order
- *              that depends on the sizes alone: the same inputs give the same bits
+ *              that depends on the sizes alone: the same inputs give the same bits. The sums of up to 768 work-groups are formed in fp32
+ *              and joined in 64 bits
  *   workspace  device, 16-byte aligned, okvq_norm_rotary_workspace_bytes(batch, n_tokens) bytes */
 okvq_status okvq_norm_rotary_backward(const okvq_rotary_params* params, int32_t batch, int32_t q_heads, int32_t kv_heads,
                                       int32_t n_tokens, const okvq_rows* q, const okvq_rows* k, const float* q_weight,
@@ -607,7 +608,7 @@ okvq_status okvq_q8_append(const okvq_q8_cache* cache, int32_t layer, const int3
 
 /* Device workspace bytes that okvq_q8_attention and okvq_q8_window_attention need for sequences up to max_seq_len and up to
  * n_max rows (0 for invalid arguments). Enough for every shorter call too (up to 16 rows of a KV head 4.3 MB, up to 32 8.7 MB, beyond
- * 34.6 MB, whatever the lengths). No initial contents are needed; calls that may overlap, captured graphs among them, need one
+ * 34.6 MB, whatever the lengths; okvq_q8_attention by itself accepts 4.3 MB, 4325376 bytes, up to 32). No initial contents are needed; calls that may overlap, captured graphs among them, need one
  * each. */
 size_t okvq_q8_workspace_bytes(const okvq_q8_dims* dims, int32_t max_seq_len, int32_t n_max);
 
@@ -635,7 +636,8 @@ okvq_status okvq_q8_attention(const okvq_q8_cache* cache, int32_t layer, const i
 /* Attention of new rows with a sliding window, for layers whose rows see the newest tokens only: with p = seq_lens[b] -
  * n_new[b] + i the place of row i, it sees the tokens t <= p with t > p - window or t < sinks (the first tokens stay
  * visible). Reads those blocks of the cache alone. One token a sequence, a chunk or a whole prompt; the arguments and the
- * workspace are those of okvq_q8_attention (okvq_q8_workspace_bytes), and
+ * workspace are those of okvq_q8_attention (okvq_q8_workspace_bytes), and so are its roundings and ranges (the softmax weights times a
+ * block's value scale in fp16, which rows that see few tokens show most), and
  *   window      1 or more: tokens that a row sees, its own among them
  *   sinks       0 or more */
 okvq_status okvq_q8_window_attention(const okvq_q8_cache* cache, int32_t layer, const int32_t* lens_host, const uint16_t* q,
@@ -646,8 +648,9 @@ okvq_status okvq_q8_window_attention(const okvq_q8_cache* cache, int32_t layer, 
 /* drafts of a slot in one call at most */
 enum { OKVQ_Q8_MAX_DRAFTS = 256 };
 
-/* Device workspace bytes that okvq_q8_tree_attention needs for up to n_max drafts (0 for invalid arguments): records of 528
- * bytes for every row of a query head, and those of okvq_q8_workspace_bytes. Enough for fewer drafts too. No initial
+/* Device workspace bytes that okvq_q8_tree_attention needs for up to n_max drafts (0 for invalid arguments): those of
+ * okvq_q8_workspace_bytes, and for every slot and KV head records of 528 bytes for its n_max Hq / H query columns, rounded up to whole
+ * tiles: up to 16 columns to 16, up to 32 to 64, beyond to multiples of 256. Enough for fewer drafts too. No initial
  * contents; calls that may overlap, captured graphs among them, need one each. */
 size_t okvq_q8_tree_workspace_bytes(const okvq_q8_dims* dims, int32_t n_max);
 

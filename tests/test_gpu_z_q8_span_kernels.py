@@ -79,3 +79,21 @@ def test_trees_do_not_read_hidden_pages(fmt, s):
     _hide(c, s, [L + 1 - s.window for L in s.lens])  # of a row that names one draft
     again = _np(_tree(c, s.lens, q, k, v, visible, s.n, s.window, s.sinks))
     assert np.isfinite(want).all() and np.array_equal(again, want)
+
+
+def test_whole_attention_of_few_rows_accepts_the_small_workspace():
+    """Up to 32 rows of a KV head the windows' calls ask for twice as much."""
+    import torch
+
+    import paper_2609_11582_amd as okvq
+    small, lens, n = 512 * 16 * 528, [3000, 700], 8
+    c = _filled(2, 2, 8, lens, 64, "int8", "fp16", 199)
+    assert okvq.okvq_q8_workspace_bytes(c.dims, 3000, n) == 2 * small
+    q, n_dev = _rows(200, 2, 8, n, 128).cuda(), torch.tensor([n, 5], dtype=torch.int32, device="cuda")
+    outs = []
+    for size in (small, 2 * small):
+        ws = torch.full((small // 2 + 4096,), float("nan"), device="cuda")  # what lies behind `size` bytes is left alone
+        outs.append(torch.zeros_like(q))
+        okvq.okvq_q8_attention(c, 0, lens, q, [n, 5], n_dev, n, 128 ** -0.5, outs[-1], ws[:size // 4])
+        assert bool(ws[small // 4:].isnan().all())
+    assert torch.equal(*outs) and bool(torch.isfinite(outs[0]).all())
