@@ -31,7 +31,8 @@ struct NormRotaryArgs {
   okvq_rows q_grad, k_grad; // backward: gradients of what the forward pass wrote
   float* parts;             // backward: [kNormParts][2][128] sums of work-groups
 };
-constexpr int kNormParts = 768;   // work-groups of a backward pass at most: three to a compute unit, what their registers allow
+constexpr int kNormParts = 768;   // work-groups of a backward pass at most: three to a compute unit, what the registers of 4 and 8
+                                  // tokens allow (fp16 rows by one token fit two, but are 256 work-groups at most)
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, int dtype, int max_len, hipStream_t s);
 int norm_rotary_parts(const NormRotaryArgs& a, int max_len);  // work-groups of one of the launches of a backward pass
 // kept: work-groups whose sums hold those of earlier launches

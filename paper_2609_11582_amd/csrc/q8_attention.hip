@@ -21,7 +21,7 @@
 //    sum of p_t stays in fp32, unrounded.
 // Where rows see a window, or precede a tree (kSpan), a wave walks those blocks of its residue that some row of the tile sees, and masks
 // their tokens row by row; a tree's part always leaves records, which q8_tree.hip joins with the drafts. One token's window of
-// 1024 behind 4 sinks: 4 heads 9.6 us, 16 slots of them 9.8, one launch each (by then two blocks a wave: latency).
+// 1024 behind 4 sinks: 4 heads 9.6 us, 16 slots of them 9.8, one launch each (four or five blocks a wave, one after the other: latency).
 // Bound: memory in large calls (131072 tokens x 4 heads 25.4 us, 5.3 TB/s), latency in small ones (32768 tokens 9.0 us: 2
 // blocks a wave; 12.0 with the merge). 4 or 16 waves in place of 8 were 16 and 10 % slower on the build that took 13.4.
 #include <algorithm>

@@ -205,11 +205,12 @@ inline bool q8_wide_is_faster(int64_t rows, int64_t units16, int64_t units64, in
 // Where rows see a window or precede a tree (span), lens are the tokens that a tile walks (q8_span), and:
 // * The wide kernel, 64 columns at a time, takes what the split kernel does not (which has up to 16 rows, and beyond what the second
 //   rule above gives it) as long as its tiles find a place at once. Its time goes with the columns rounded up to 64, the
-//   prompt kernel's with those rounded up to 256, at much the same rate: 32 rows 84 -> 50 us (16 slots of 16384 tokens x 4 heads, against
-//   the split kernel), 112 rows 30 -> 23 (4 heads x 32768 tokens, against the prompt kernel), 280 rows 54 -> 37, 320 rows x 131072 tokens
-//   154 -> 108, 448 rows 56 -> 48, 512 rows x 131072 tokens 159 -> 161. With more tiles than compute units it takes more rounds,
-//   each with a start and an end, and is taken where that pays (4 heads of 128 slots: 56 rows at 2000 tokens 113 -> 80 us, 28 rows 90 -> 64;
-//   not for 112 rows, 139 and 154, nor for 28 rows at 300 tokens, 30 and 34; prompts with windows of 1024 170 and 235).
+//   prompt kernel's with those rounded up to 256, at much the same rate: 28 rows 83 -> 50 us (16 slots of 16384 tokens x 4 heads, against
+//   the split kernel), 112 rows 28 -> 23 (4 heads x 32768 tokens, against the prompt kernel), 280 rows 57 -> 37, 320 rows x 131072 tokens
+//   158 -> 111, 448 rows 57 -> 48. Where the rows fill tiles of 256 and the sequence is long it is no faster: 512 rows x 131072 tokens 160 -> 165
+//   with int8, 157 -> 153 with e4m3 (at 32768 58 -> 53 and 57 -> 50). With more tiles than compute units it takes more rounds,
+//   each with a start and an end, and is taken where that pays (4 heads of 128 slots: 56 rows at 2000 tokens 113 -> 76 us, 28 rows 88 -> 62;
+//   not for 112 rows, 134 and 148, nor for 28 rows at 300 tokens, 30 and 33; prompts with windows of 1024 171 and 240).
 // * The prompt kernel's tiles of 128 columns where short windows leave compute units idle, or take more than one round of tiles of
 //   256, whose last one is seldom full: two work-groups share a compute unit and end one by one (8192 rows x 28 heads, window 1024: 896
 //   tiles 192 -> 175 us; 1024 tiles, 4 full rounds, 196 -> 194; 256 tiles, one round, 49 -> 55). Windows of 2000 and more: 5 % slower.

@@ -1,8 +1,8 @@
 // Attention of drafted trees, the drafts' part: joins the splits of the cache's part with it.
 //
 // A row's softmax runs over the cache's tokens and the drafts that its mask names (its ancestors and itself, a few). The
-// split and prompt kernels leave records (M, m, l, sums) of the cache's part (q8_attention.hip); here a work-group takes one
-// query column, attends its drafts in fp32 from their rows as they are, with a running maximum, and adds all parts: as a
+// split, wide and prompt kernels leave records (M, m, l, sums) of the cache's part (q8_attention.hip); here a work-group takes 1 to 8
+// query columns, attends their drafts in fp32 from their rows as they are, with a running maximum, and adds all parts: as a
 // record the drafts' part has m, l and sums 2^-8 p v, whose reference M is m + kWeightExp + 8 (256 values of bfloat16's
 // largest size stay finite).
 //
